@@ -1,0 +1,524 @@
+"""Workloads that time the page operators and the 8-bit latent cache, through the package's public entry points or, as a yardstick,
+in elementary torch operations.
+
+What surrounds decode attention in a serving loop: a prompt is answered several times (its pages are shared, the last one copied),
+users leave and others arrive (pages freed, the pool made dense, pages given out), prompts and new tokens move into the 8-bit cache,
+and every step attends to it.
+
+Shapes are those of this repository's other workloads: the 8B layer (D 4096, 32 query / 8 KV heads of 128), the 70B layer (D 8192,
+64 / 8) and the tiny layer of the smoke test.  Latents are N(0, sigma_j^2) with the power-law spectrum sigma_j ~ j^-0.7, keys and
+values of an uncompressed layer and queries N(0, 1).
+"""
+import math
+
+import torch
+
+own = False
+
+PAGE = 64    # positions per page
+GROUP = 128  # latents that share a scale in the 8-bit cache
+
+SHAPES = {
+    "tiny": dict(d_model=256, q_heads=4, kv_heads=2, head_dim=64, rope_base=10000.0),
+    "8b": dict(d_model=4096, q_heads=32, kv_heads=8, head_dim=128, rope_base=500000.0),
+    "70b": dict(d_model=8192, q_heads=64, kv_heads=8, head_dim=128, rope_base=500000.0),
+}
+
+
+def _case(kind, shape, rank, batch, context, *, ragged=False, fan=0, eight_bits=False, name=None):
+    """kind: "fork" (every sequence continued `fan` times), "turnover" (a third of the sequences leave, the pool is made dense, as
+    many arrive), "quantize" (prompts into the 8-bit cache), "quantize_tokens" (the newest token of every sequence), "decode",
+    "decode_plain" (uncompressed layer), "decode_absorbed" (no rotation).  context: the longest sequence; ragged: the others are
+    shorter, down to an eighth of it.  eight_bits: the pages that are moved are the 8-bit cache's."""
+    c = dict(kind=kind, shape=shape, rank=rank, batch=batch, context=context, ragged=ragged, fan=fan, eight_bits=eight_bits)
+    if name is not None:
+        c["name"] = name
+    return c
+
+
+def listed():
+    return [
+        # four answers to one prompt: all latency
+        _case("fork", "8b", 512, 1, 777, fan=4, name="fork_answers"),
+        # four samples of each of 64 conversations, each at another length
+        _case("fork", "8b", 512, 64, 8192, ragged=True, fan=4, name="fork_batch"),
+        # a small pool, a few short sequences
+        _case("turnover", "tiny", 32, 6, 300, ragged=True, name="turnover_tiny"),
+        # a full pool of 8-bit pages when a third of the users leaves
+        _case("turnover", "8b", 512, 128, 8192, ragged=True, eight_bits=True, name="turnover_pool"),
+        # a decode step's new tokens
+        _case("quantize_tokens", "8b", 512, 64, 4096, ragged=True, name="quantize_tokens"),
+        # the benchmark's prompts
+        _case("quantize", "8b", 512, 4, 8192, name="quantize_prompts"),
+        # one interactive user of an uncompressed layer
+        _case("decode_plain", "8b", 1024, 1, 1337, name="plain_single_user"),
+        # an uncompressed layer, sixteen users
+        _case("decode_plain", "8b", 1024, 16, 4096, name="plain_batch16"),
+        # no rotation: a few users, ordinary lengths that are multiples of nothing
+        _case("decode_absorbed", "8b", 384, 3, 1999, ragged=True, name="absorbed_few_users"),
+        # no rotation, sixteen users
+        _case("decode_absorbed", "8b", 512, 16, 8192, name="absorbed_batch16"),
+        # the smoke test's layer: one short sequence
+        _case("decode", "tiny", 32, 1, 128, name="decode_tiny"),
+        # the headline decode step: sixteen users, 4096 positions each
+        _case("decode", "8b", 512, 16, 4096, name="decode_batch16"),
+    ]
+
+
+# ------------------------------------------------------------------------------------------------ sizes of a case
+def _lengths(case):
+    """Positions per sequence: the first has `context`; ragged ones are spread over [context / 8, context]."""
+    n, out = case["context"], []
+    for s in range(case["batch"]):
+        short = 0.875 * ((s * 0.6180339887498949) % 1.0) if case["ragged"] else 0.0
+        out.append(max(1, int(n * (1.0 - short))))
+    return out
+
+
+def _pages(length):
+    return (length + PAGE - 1) // PAGE
+
+
+def _groups(r):
+    return (r + GROUP - 1) // GROUP
+
+
+def _page_bytes(r, eight_bits):
+    return PAGE * (2 * r + 2 * _groups(r)) if eight_bits else 4 * PAGE * r
+
+
+def _leaving(case):
+    """Rows that leave, and the lengths of those that take their place."""
+    rows = list(range(0, case["batch"], 3))
+    lens = _lengths(case)
+    return rows, [max(1, (lens[s] * 5) // 7) for s in rows]
+
+
+def work(case):
+    """Fork and turnover: page ids, references and moved pages, read and written once.  Quantize: latents read, codes and scales
+    written.  Decode: codes, scales, factors and queries read once, outputs written; operations as in attention over latents."""
+    sh, r, lens = SHAPES[case["shape"]], case["rank"], _lengths(case)
+    hq, d = sh["q_heads"], sh["head_dim"]
+    n, kind = sh["kv_heads"] * d, case["kind"]
+    pages = [_pages(L) for L in lens]
+    if kind == "fork":
+        tails = sum(case["fan"] for L in lens if L % PAGE)
+        return {"bytes": 2 * tails * _page_bytes(r, case["eight_bits"]) + 4 * sum(p * (1 + 3 * case["fan"]) for p in pages), "flops": 0}
+    if kind == "turnover":
+        rows, arrive = _leaving(case)
+        gone = sum(pages[s] for s in rows)
+        moved = gone * (sum(pages) - gone) // max(1, sum(pages))
+        ids = sum(pages) + gone + sum(_pages(L) for L in arrive)
+        return {"bytes": 2 * moved * _page_bytes(r, case["eight_bits"]) + 8 * ids + 8 * sum(pages), "flops": 0}
+    per_position = 2 * r + 2 * _groups(r)
+    if kind.startswith("quantize"):
+        new = sum(lens) if kind == "quantize" else case["batch"]
+        return {"bytes": new * (4 * r + per_position), "flops": 4 * new * r}
+    positions, b = sum(lens), case["batch"]
+    score_width = r if kind == "decode_absorbed" else d
+    nbytes = positions * per_position + 2 * b * hq * (score_width + d) + 4 * sum(pages)
+    if kind == "decode_plain":
+        return {"bytes": nbytes, "flops": 4 * hq * d * positions}
+    nbytes += 2 * r * n * (1 if kind == "decode_absorbed" else 2)
+    flops = 2 * hq * (score_width + r) * positions + 2 * b * hq * r * d
+    if kind == "decode":
+        flops += 2 * r * n * positions
+    return {"bytes": nbytes, "flops": flops}
+
+
+def draw(rng):
+    log_int = lambda lo, hi: int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))  # noqa: E731
+    most = {}
+    for w, c in ((work(c), c) for c in listed()):
+        m = most.setdefault(c["kind"], [0, 0])
+        most[c["kind"]] = [max(m[0], w["bytes"]), max(m[1], w["flops"])]
+    most["quantize_tokens"] = most["quantize"]
+    kind = rng.choice(["fork", "turnover", "quantize", "quantize_tokens", "decode", "decode", "decode_plain", "decode_absorbed"])
+    shape = rng.choice(["8b", "8b", "8b", "70b", "tiny"] if kind != "decode_plain" else ["8b", "8b", "70b"])
+    rank = 1024 if kind == "decode_plain" else {"tiny": 32 * rng.randint(1, 4), "8b": 32 * rng.randint(4, 16), "70b": 32 * rng.randint(6, 16)}[shape]
+    batch = log_int(1, 128 if kind in ("fork", "turnover", "quantize_tokens") else 32)
+    case = _case(kind, shape, rank, batch, log_int(2, 16384), ragged=rng.random() < 0.7, fan=rng.randint(1, 8) if kind == "fork" else 0,
+                 eight_bits=kind in ("fork", "turnover") and rng.random() < 0.5)
+    while any(w > m for w, m in zip((work(case)["bytes"], work(case)["flops"]), most[kind])):
+        case["context"] = max(1, case["context"] * 3 // 4)
+        case["batch"] = max(1, case["batch"] * 7 // 8)
+    return case
+
+
+# ------------------------------------------------------------------------------------------------ layouts (plain form)
+# K latent j of slot t: ((t/32 * (r/16) + j/16) * 64 + t%32 + 32*((j%16)/8)) * 8 + j%8
+# V latent j of slot t: ((j/32 * 4 + t/16) * 64 + j%32 + 32*((t%16)/8)) * 8 + t%8,  behind the 64 r elements of the K part
+def _to_page(v, keys):
+    """[pages, 64, r] in order of position and latent -> [pages, 64 r] in the page's order."""
+    p, _, r = v.shape
+    if keys:
+        return v.view(p, 2, 32, r // 16, 2, 8).permute(0, 1, 3, 4, 2, 5).reshape(p, PAGE * r)
+    return v.view(p, 4, 2, 8, r // 32, 32).permute(0, 4, 1, 2, 5, 3).reshape(p, PAGE * r)
+
+
+def _from_page(v, keys):
+    """The inverse of _to_page."""
+    p, r = v.shape[0], v.shape[1] // PAGE
+    if keys:
+        return v.reshape(p, 2, r // 16, 2, 32, 8).permute(0, 1, 4, 2, 3, 5).reshape(p, PAGE, r)
+    return v.reshape(p, r // 32, 4, 2, 32, 8).permute(0, 2, 3, 5, 1, 4).reshape(p, PAGE, r)
+
+
+def _split(pool, r):
+    """An 8-bit pool [pages, page bytes] as codes of K and V [pages, 64 r] and scale bytes [pages, groups, 64]."""
+    g = _groups(r)
+    scales = pool[:, 2 * PAGE * r:].view(pool.shape[0], 2 * g, PAGE)
+    return pool[:, :PAGE * r], pool[:, PAGE * r:2 * PAGE * r], scales[:, :g], scales[:, g:]
+
+
+def _encode(x):
+    """[..., r] float32 -> e4m3 codes and scale bytes [..., groups]."""
+    r = x.shape[-1]
+    padded = torch.nn.functional.pad(x, (0, _groups(r) * GROUP - r)).unflatten(-1, (-1, GROUP))
+    most = torch.where(torch.isfinite(padded), padded.abs(), torch.zeros_like(padded)).amax(-1)
+    m, e = torch.frexp(most)
+    k = (e - 8 - (m <= 0.875).to(e.dtype)).clamp(-126, 127)
+    k = torch.where(most > 0, k, torch.full_like(k, -126))
+    inv = torch.ldexp(torch.ones_like(most), -k)
+    codes = (padded * inv.unsqueeze(-1)).flatten(-2)[..., :r].to(torch.float8_e4m3fn)
+    return codes, (k + 127).to(torch.uint8)
+
+
+def _values(codes, scale_bytes, keys):
+    """Codes [pages, 64 r] and scale bytes [pages, groups, 64] -> float32 [pages, 64, r]."""
+    x = _from_page(codes.view(torch.float8_e4m3fn).float(), keys)
+    k = scale_bytes.to(torch.int32).transpose(1, 2) - 127
+    return x * torch.ldexp(torch.ones_like(k, dtype=torch.float32), k).repeat_interleave(GROUP, dim=2)[:, :, :x.shape[2]]
+
+
+# ------------------------------------------------------------------------------------------------ inputs
+def prepare(case, seed):
+    dev = torch.device("cuda")
+    rng = torch.Generator(device=dev).manual_seed(1000003 * (seed + 1))
+    host = torch.Generator().manual_seed(seed + 17)
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device=dev)  # noqa: E731
+    kind, r, lens, batch = case["kind"], case["rank"], _lengths(case), case["batch"]
+    sh = SHAPES[case["shape"]]
+    hq, hkv, d = sh["q_heads"], sh["kv_heads"], sh["head_dim"]
+    n = hkv * d
+    sigma = torch.arange(1, n + 1, device=dev, dtype=torch.float64) ** -0.7
+    sigma = (sigma * math.sqrt(n) / sigma.norm()).float()[:r]
+    if kind == "decode_plain":
+        sigma = torch.ones_like(sigma)
+    max_pages = max(_pages(L) for L in lens) + 1
+    held = [_pages(L) for L in lens]
+    extra = {"fork": case["fan"] * batch + 2, "turnover": 2 + sum(_pages(L) for L in _leaving(case)[1]) // 2}.get(kind, 3)
+    n_pages = sum(held) + extra
+    order = torch.randperm(n_pages, generator=host)
+    rows = batch * (1 + case["fan"])
+    entry = torch.arange(max_pages).view(1, -1)
+    first = torch.tensor([0] + held).cumsum(0)[:-1].view(-1, 1)
+    mapped = entry < torch.tensor(held).view(-1, 1)
+    table = torch.full((rows, max_pages), -1, dtype=torch.int64)
+    table[:batch] = torch.where(mapped, order[(first + entry).clamp(max=n_pages - 1)], torch.tensor(-1))
+    refs = torch.zeros(n_pages, dtype=torch.int32)
+    refs[table[table >= 0]] = 1
+    st = dict(kind=kind, shape=sh, r=r, block_table=table.to(torch.int32).to(dev), n_pages=n_pages)
+
+    if kind in ("fork", "turnover"):
+        st["pool"] = torch.randint(-2 ** 31, 2 ** 31 - 1, (n_pages, _page_bytes(r, case["eight_bits"]) // 4), dtype=torch.int32, device=dev, generator=rng)
+        st["table0"], st["refs0"], st["page_refs"] = st["block_table"].clone(), refs.to(dev), refs.to(dev)
+        if kind == "fork":
+            pairs = batch * case["fan"]
+            st["parents"] = i32([i // case["fan"] for i in range(pairs)])
+            st["children"], st["lens"] = i32(list(range(batch, rows))), i32([lens[i // case["fan"]] for i in range(pairs)])
+            slots = pairs
+        else:
+            gone, arrive = _leaving(case)
+            st["gone"], st["lens"] = i32(gone), i32(arrive)
+            slots, st["page_map"] = n_pages // 2, torch.empty(n_pages, dtype=torch.int32, device=dev)
+        st["copy_src"], st["copy_dst"] = (torch.empty(slots, dtype=torch.int32, device=dev) for _ in range(2))
+        st["status"] = torch.empty_like(st["lens"])
+        if own:  # scratch memory that such a program keeps
+            import paper_2410_03111_amd as lorc
+            st["workspace"] = torch.empty(lorc.pages_workspace_bytes(rows, n_pages), dtype=torch.uint8, device=dev)
+        return st
+
+    desc_args = (sh["d_model"], hq, hkv, d, r, r, sh["rope_base"])
+    if own:
+        import paper_2410_03111_amd as lorc
+        st["desc"] = lorc.layer_desc(*desc_args)
+    if kind.startswith("quantize"):
+        scale = torch.cat([_to_page(sigma.view(1, 1, r).expand(1, PAGE, r), keys) for keys in (True, False)], 1).view(-1)
+        st["cache"] = torch.randn(n_pages, 2 * PAGE * r, generator=rng, device=dev).mul_(scale).to(torch.bfloat16)
+        st["table_q8"] = torch.where(table >= 0, torch.randperm(n_pages, generator=host)[table.clamp(min=0)], table).to(torch.int32).to(dev)
+        st["cache_q8"] = torch.zeros(n_pages, _page_bytes(r, True), dtype=torch.uint8, device=dev)
+        st["pos_end"] = i32(lens)
+        st["pos_begin"] = i32([0] * batch if kind == "quantize" else [L - 1 for L in lens])
+        st["max_tokens"] = max(lens) if kind == "quantize" else 1
+        return st
+
+    pool = torch.empty(n_pages, _page_bytes(r, True), dtype=torch.uint8, device=dev)
+    chunk = max(1, (1 << 27) // (PAGE * r))
+    for p0 in range(0, n_pages, chunk):
+        part = pool[p0:p0 + chunk]
+        for where, scales, keys in ((slice(0, PAGE * r), 0, True), (slice(PAGE * r, 2 * PAGE * r), 1, False)):
+            codes, s = _encode(torch.randn(part.shape[0], PAGE, r, generator=rng, device=dev).mul_(sigma).to(torch.bfloat16).float())
+            part[:, where] = _to_page(codes.view(torch.uint8), keys)
+            g = _groups(r) * PAGE
+            part[:, 2 * PAGE * r + scales * g:2 * PAGE * r + (scales + 1) * g] = s.transpose(1, 2).reshape(part.shape[0], g)
+    st.update(cache_q8=pool, ctx_len=i32(lens), q_pos=i32([L - 1 for L in lens]), max_ctx=max(lens),
+              q=torch.randn(batch, hq, d, generator=rng, device=dev).to(torch.bfloat16),
+              out=torch.empty(batch, hq, d, dtype=torch.bfloat16, device=dev))
+    A = [torch.randn(sh["d_model"], r, generator=rng, device=dev).mul_(sigma / math.sqrt(sh["d_model"])).to(torch.bfloat16) for _ in range(2)]
+    B = [None, None]
+    if kind != "decode_plain":
+        B = [torch.randn(r, n, generator=rng, device=dev).mul_(1 / math.sqrt(n)).to(torch.bfloat16) for _ in range(2)]
+    if kind == "decode_absorbed":
+        per_head = B[0].float().view(r, hkv, d).permute(1, 2, 0).contiguous()
+        st["q"] = torch.matmul(st["q"].float().view(batch, hkv, hq // hkv, d), per_head).view(batch, hq, r).to(torch.bfloat16).contiguous()
+    st["B_k"], st["B_v"] = B
+    if own:  # packed factors and workspace, laid out once
+        size = {"decode": lorc.decode_q8_workspace_bytes, "decode_plain": lorc.decode_plain_q8_workspace_bytes,
+                "decode_absorbed": lorc.decode_absorbed_q8_workspace_bytes}[kind]
+        st["packed"] = lorc.pack_factors(st["desc"], A[0], A[1], B[0], B[1])
+        st["workspace"] = torch.empty(size(st["desc"], batch, max(lens)), dtype=torch.uint8, device=dev)
+    return st
+
+
+# ------------------------------------------------------------------------------------------------ a pass
+def run(st):
+    kind = st["kind"]
+    if kind in ("fork", "turnover"):
+        st["block_table"].copy_(st["table0"])  # the same tables before every pass
+        st["page_refs"].copy_(st["refs0"])
+    if own:
+        return _run_own(st, kind)
+    if kind == "fork":
+        return _plain_fork(st)
+    if kind == "turnover":
+        return _plain_turnover(st)
+    if kind.startswith("quantize"):
+        return _plain_quantize(st)
+    return _plain_decode(st, kind)
+
+
+def _moved(st, *more):
+    return {k: st[k] for k in ("block_table", "page_refs", "copy_src", "copy_dst", "status", "pool") + more}
+
+
+def _codes(st):
+    at = 2 * PAGE * st["r"]
+    return {"codes": st["cache_q8"][:, :at].view(torch.float8_e4m3fn), "scales": st["cache_q8"][:, at:]}
+
+
+def _run_own(st, kind):
+    import paper_2410_03111_amd as lorc
+    if kind == "fork":
+        lorc.fork_sequences(st["block_table"], st["page_refs"], st["parents"], st["children"], st["lens"], st["copy_src"], st["copy_dst"],
+                            st["status"], workspace=st["workspace"])
+        lorc.copy_pages(st["pool"], st["copy_src"], st["copy_dst"])
+        return _moved(st)
+    if kind == "turnover":
+        lorc.free_sequences(st["block_table"], st["page_refs"], st["gone"])
+        lorc.compact_pages(st["block_table"], st["page_refs"], st["copy_src"], st["copy_dst"], st["page_map"], workspace=st["workspace"])
+        lorc.copy_pages(st["pool"], st["copy_src"], st["copy_dst"])
+        lorc.reserve_pages(st["block_table"], st["page_refs"], st["gone"], st["lens"], st["status"], workspace=st["workspace"])
+        return _moved(st, "page_map")
+    if kind.startswith("quantize"):
+        lorc.quantize_latents(st["desc"], st["cache"], st["block_table"], st["pos_begin"], st["pos_end"], st["max_tokens"],
+                              st["cache_q8"], st["table_q8"])
+        return _codes(st)
+    if kind == "decode_absorbed":
+        lorc.decode_attention_absorbed_q8(st["desc"], st["q"], st["ctx_len"], st["max_ctx"], st["packed"], st["cache_q8"], st["block_table"],
+                                          out=st["out"], workspace=st["workspace"])
+    else:
+        attend = lorc.decode_attention_plain_q8 if kind == "decode_plain" else lorc.decode_attention_q8
+        attend(st["desc"], st["q"], st["q_pos"], st["ctx_len"], st["max_ctx"], st["packed"], st["cache_q8"], st["block_table"],
+               out=st["out"], workspace=st["workspace"])
+    return {"out": st["out"]}
+
+
+def _plain_fork(st):
+    table, refs, parents, children, lens = st["block_table"], st["page_refs"], st["parents"].long(), st["children"].long(), st["lens"].long()
+    entry = torch.arange(table.shape[1], device=table.device).view(1, -1)
+    whole = entry < (lens // PAGE).view(-1, 1)
+    rows = table[parents]
+    tail = lens % PAGE != 0
+    free = torch.nonzero(refs == 0).view(-1)
+    rank = tail.long().cumsum(0) - 1
+    served = ~tail | (rank < free.numel())
+    fresh = free[rank.clamp(0, max(0, free.numel() - 1))]
+    takes = tail & served
+    refs += torch.bincount(rows[whole & served.view(-1, 1)].long(), minlength=refs.numel()).to(refs.dtype)
+    refs[fresh[takes]] = 1
+    new = torch.where(whole, rows, torch.full_like(rows, -1))
+    at_tail = takes.view(-1, 1) & (entry == (lens // PAGE).view(-1, 1))
+    new = torch.where(at_tail, fresh.view(-1, 1).to(new.dtype), new)
+    table[children] = torch.where(served.view(-1, 1), new, torch.full_like(new, -1))
+    source = rows.gather(1, (lens // PAGE).clamp(max=table.shape[1] - 1).view(-1, 1)).view(-1)
+    st["copy_src"].copy_(torch.where(takes, source, torch.full_like(source, -1)))
+    st["copy_dst"].copy_(torch.where(takes, fresh.to(source.dtype), torch.full_like(source, -1)))
+    st["status"].copy_(torch.where(served, 0, 2))
+    _plain_copy(st)
+    return _moved(st)
+
+
+def _plain_copy(st):
+    ok = st["copy_dst"] >= 0
+    st["pool"][st["copy_dst"][ok].long()] = st["pool"][st["copy_src"][ok].long()]
+
+
+def _plain_turnover(st):
+    table, refs, gone, lens = st["block_table"], st["page_refs"], st["gone"].long(), st["lens"].long()
+    # free
+    left = table[gone]
+    refs -= torch.bincount(left[left >= 0].long(), minlength=refs.numel()).to(refs.dtype)
+    table[gone] = -1
+    # compact
+    holes, used = torch.nonzero(refs == 0).view(-1), torch.nonzero(refs > 0).view(-1).flip(0)
+    m = min(holes.numel(), used.numel(), st["copy_src"].numel())
+    ok = holes[:m] < used[:m]
+    src, dst = used[:m][ok], holes[:m][ok]
+    st["copy_src"].fill_(-1)
+    st["copy_dst"].fill_(-1)
+    st["copy_src"][:src.numel()] = src.to(torch.int32)
+    st["copy_dst"][:dst.numel()] = dst.to(torch.int32)
+    st["page_map"].copy_(torch.arange(refs.numel(), device=refs.device))
+    st["page_map"][src] = dst.to(torch.int32)
+    refs[dst] = refs[src]
+    refs[src] = 0
+    table.copy_(torch.where(table >= 0, st["page_map"][table.clamp(min=0).long()], table))
+    _plain_copy(st)
+    # reserve
+    rows = table[gone]
+    entry = torch.arange(table.shape[1], device=table.device).view(1, -1)
+    missing = (entry < ((lens + PAGE - 1) // PAGE).view(-1, 1)) & (rows < 0)
+    count = missing.sum(1)
+    before = count.cumsum(0) - count
+    free = torch.nonzero(refs == 0).view(-1)
+    served = before + count <= free.numel()
+    takes = missing & served.view(-1, 1)
+    page = free[(before.view(-1, 1) + missing.long().cumsum(1) - 1).clamp(0, free.numel() - 1)]
+    table[gone] = torch.where(takes, page.to(rows.dtype), rows)
+    refs[page[takes]] = 1
+    st["status"].copy_(torch.where(served, 0, 2))
+    return _moved(st, "page_map")
+
+
+def _plain_quantize(st):
+    r, pool = st["r"], st["cache_q8"]
+    dev = pool.device
+    pos = st["pos_begin"].view(-1, 1).long() + torch.arange(st["max_tokens"], device=dev)
+    seq, tok = torch.nonzero(pos < st["pos_end"].view(-1, 1), as_tuple=True)
+    pos = pos[seq, tok]
+    src, dst = (t[seq, pos // PAGE].long().view(-1, 1) for t in (st["block_table"], st["table_q8"]))
+    t, j = (pos % PAGE).view(-1, 1), torch.arange(r, device=dev).view(1, -1)
+    at_k = ((t // 32 * (r // 16) + j // 16) * 64 + t % 32 + 32 * (j % 16 // 8)) * 8 + j % 8
+    at_v = ((j // 32 * 4 + t // 16) * 64 + j % 32 + 32 * (t % 16 // 8)) * 8 + t % 8 + PAGE * r
+    g = torch.arange(_groups(r), device=dev).view(1, -1)
+    for at, first in ((at_k, 0), (at_v, _groups(r))):
+        codes, scales = _encode(st["cache"][src, at].float())
+        pool[dst, at] = codes.view(torch.uint8)
+        pool[dst, 2 * PAGE * r + (first + g) * PAGE + t] = scales
+    return _codes(st)
+
+
+def _turn(x, cos, sin):
+    lo, hi = x.chunk(2, dim=-1)
+    return torch.cat([lo * cos - hi * sin, hi * cos + lo * sin], dim=-1)
+
+
+def _plain_decode(st, kind):
+    sh, r, table, q = st["shape"], st["r"], st["block_table"], st["q"].float()
+    hkv, d = sh["kv_heads"], sh["head_dim"]
+    b, G, max_ctx = q.shape[0], sh["q_heads"] // hkv, st["max_ctx"]
+    ids = table[:b, :_pages(max_ctx)]
+    mapped = ids >= 0
+    k_codes, v_codes, k_scales, v_scales = (t[ids.clamp(min=0).reshape(-1).long()] for t in _split(st["cache_q8"], r))
+    zero = mapped.view(-1, 1, 1).float()
+    c_k = (_values(k_codes, k_scales, True) * zero).view(b, -1, r)
+    c_v = (_values(v_codes, v_scales, False) * zero).view(b, -1, r)
+    pos = torch.arange(c_k.shape[1], device=q.device)
+    seen = pos.view(1, 1, -1) < st["ctx_len"].view(b, 1, 1)
+    if kind == "decode_absorbed":
+        s = torch.matmul(q, c_k.transpose(1, 2).contiguous())
+    else:
+        K = c_k if kind == "decode_plain" else torch.matmul(c_k.view(-1, r), st["B_k"].float())
+        K = K.view(b, -1, hkv, d).transpose(1, 2)
+        theta = sh["rope_base"] ** (-2.0 * torch.arange(d // 2, device=q.device, dtype=torch.float64) / d)
+        a_k, a_q = pos.double().view(-1, 1) * theta, st["q_pos"].double().view(b, 1, 1) * theta
+        K = _turn(K, a_k.cos().float(), a_k.sin().float())
+        q = _turn(q, a_q.cos().float(), a_q.sin().float())
+        s = torch.matmul(q.view(b, hkv, G, d), K.transpose(2, 3).contiguous()).view(b, hkv * G, -1)
+    s = torch.where(seen, s / math.sqrt(d), torch.full_like(s, float("-inf")))
+    p = torch.exp(s - s.amax(-1, keepdim=True))
+    p = p / p.sum(-1, keepdim=True)
+    if kind == "decode_plain":
+        V = c_v.view(b, -1, hkv, d).transpose(1, 2).contiguous()
+        o = torch.matmul(p.view(b, hkv, G, -1), V)
+    else:
+        o = torch.matmul(torch.matmul(p, c_v).view(b, hkv, G, r), st["B_v"].float().view(r, hkv, d).transpose(0, 1).contiguous())
+    st["out"].copy_(o.reshape(b, hkv * G, d))
+    return {"out": st["out"]}
+
+
+# ------------------------------------------------------------------------------------------------ definition in 64 bits
+def _value_of_code(c):
+    """e4m3: sign, four exponent bits (bias 7), three bits of fraction; exponent 0 has no leading one."""
+    c = c.long()
+    e, f = (c >> 3) & 15, (c & 7).double()
+    mag = torch.where(e == 0, f * 2.0 ** -9, (8 + f) * torch.exp2((e - 10).double()))
+    return torch.where(c >= 128, -mag, mag)
+
+
+def exact(case, seed):
+    st = prepare(case, seed)
+    kind, r, table = st["kind"], st["r"], st["block_table"]
+    if kind in ("fork", "turnover"):
+        return None  # page ids and copies: nothing is rounded
+    dev = table.device
+    j = torch.arange(r, device=dev).view(1, -1)
+    t = torch.arange(PAGE, device=dev).view(-1, 1)
+    at = [((t // 32 * (r // 16) + j // 16) * 64 + t % 32 + 32 * (j % 16 // 8)) * 8 + j % 8,
+          ((j // 32 * 4 + t // 16) * 64 + j % 32 + 32 * (t % 16 // 8)) * 8 + t % 8 + PAGE * r]
+    if kind.startswith("quantize"):
+        codes = torch.zeros(st["n_pages"], 2 * PAGE * r, dtype=torch.float64, device=dev)
+        for s in range(case["batch"]):
+            for page in range(int(st["pos_begin"][s]) // PAGE, _pages(int(st["pos_end"][s]))):
+                pos = page * PAGE + t
+                new = (pos >= st["pos_begin"][s]) & (pos < st["pos_end"][s])
+                src, dst = int(table[s, page]), int(st["table_q8"][s, page])
+                for part in range(2):
+                    x = st["cache"][src].double()[at[part]]
+                    most = torch.cat([x[:, g:g + GROUP].abs().amax(1, keepdim=True).expand(-1, min(GROUP, r - g)) for g in range(0, r, GROUP)], 1)
+                    scale = torch.exp2(torch.ceil(torch.log2(most / 448.0)))  # (exact where it matters: bf16 / 448 is no power of two but 448 2^k)
+                    y = x / scale
+                    step = torch.exp2(torch.floor(torch.log2(y.abs().clamp(min=2.0 ** -6))) - 3)
+                    y = torch.round(y / step) * step
+                    codes[dst][at[part]] = torch.where(new, y, codes[dst][at[part]])
+        return {"codes": codes, "scales": None}
+    sh = st["shape"]
+    hkv, d, G, base = sh["kv_heads"], sh["head_dim"], sh["q_heads"] // sh["kv_heads"], sh["rope_base"]
+    out = torch.zeros(case["batch"], hkv * G, d, dtype=torch.float64, device=dev)
+    pool, f64 = st["cache_q8"], torch.float64
+    theta = torch.tensor([base ** (-2.0 * i / d) for i in range(d // 2)], dtype=f64, device=dev)
+
+    def rotate(x, pos):  # [..., d] at positions [...]
+        z = torch.complex(x[..., :d // 2].contiguous(), x[..., d // 2:].contiguous()) * torch.polar(torch.ones_like(pos * theta), pos * theta)
+        return torch.cat([z.real, z.imag], -1)
+
+    for s in range(case["batch"]):
+        L = int(st["ctx_len"][s])
+        pages = pool[table[s, :_pages(L)].long()]
+        c = []
+        for part in range(2):
+            scale = pages[:, 2 * PAGE * r + (part * _groups(r) + j // GROUP) * PAGE + t].double() - 127
+            c.append((_value_of_code(pages[:, at[part]]) * torch.exp2(scale)).view(-1, r)[:L])
+        pos = torch.arange(L, device=dev, dtype=f64).view(-1, 1, 1)
+        if kind == "decode_absorbed":
+            w = st["q"][s].to(f64) @ c[0].T
+        else:
+            K = (c[0] if kind == "decode_plain" else c[0] @ st["B_k"].to(f64)).view(L, hkv, d)
+            K, q = rotate(K, pos), rotate(st["q"][s].to(f64), torch.tensor(float(L - 1), dtype=f64, device=dev))
+            w = torch.stack([K[:, h // G] @ q[h] for h in range(hkv * G)])
+        w = torch.softmax(w / math.sqrt(d), -1)
+        for h in range(hkv * G):
+            cols = slice(h // G * d, (h // G + 1) * d)
+            out[s, h] = w[h] @ c[1][:, cols] if kind == "decode_plain" else (w[h] @ c[1]) @ st["B_v"][:, cols].to(f64)
+    return {"out": out}
