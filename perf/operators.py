@@ -245,7 +245,7 @@ def prepare(case, seed):
         st["desc"] = lorc.layer_desc(*desc_args)
     if kind.startswith("quantize"):
         scale = torch.cat([_to_page(sigma.view(1, 1, r).expand(1, PAGE, r), keys) for keys in (True, False)], 1).view(-1)
-        st["cache"] = torch.randn(n_pages, 2 * PAGE * r, generator=rng, device=dev).mul_(scale).to(torch.bfloat16)
+        st["cache"] = torch.randn(n_pages, 2 * PAGE * r, generator=rng, device=dev).mul_(scale).to(torch.bfloat16).view(torch.uint8)
         st["table_q8"] = torch.where(table >= 0, torch.randperm(n_pages, generator=host)[table.clamp(min=0)], table).to(torch.int32).to(dev)
         st["cache_q8"] = torch.zeros(n_pages, _page_bytes(r, True), dtype=torch.uint8, device=dev)
         st["pos_end"] = i32(lens)
@@ -274,8 +274,8 @@ def prepare(case, seed):
         st["q"] = torch.matmul(st["q"].float().view(batch, hkv, hq // hkv, d), per_head).view(batch, hq, r).to(torch.bfloat16).contiguous()
     st["B_k"], st["B_v"] = B
     if own:  # packed factors and workspace, laid out once
-        size = {"decode": lorc.decode_q8_workspace_bytes, "decode_plain": lorc.decode_plain_q8_workspace_bytes,
-                "decode_absorbed": lorc.decode_absorbed_q8_workspace_bytes}[kind]
+        size = {"decode": lorc.decode_quantized_workspace_bytes, "decode_plain": lorc.decode_plain_quantized_workspace_bytes,
+                "decode_absorbed": lorc.decode_absorbed_quantized_workspace_bytes}[kind]
         st["packed"] = lorc.pack_factors(st["desc"], A[0], A[1], B[0], B[1])
         st["workspace"] = torch.empty(size(st["desc"], batch, max(lens)), dtype=torch.uint8, device=dev)
     return st
@@ -316,7 +316,7 @@ def _run_own(st, kind):
         return _moved(st)
     if kind == "turnover":
         lorc.free_sequences(st["block_table"], st["page_refs"], st["gone"])
-        lorc.compact_pages(st["block_table"], st["page_refs"], st["copy_src"], st["copy_dst"], st["page_map"], workspace=st["workspace"])
+        lorc.compact_pages(st["block_table"], st["page_refs"], st["copy_src"], st["copy_dst"], st["page_map"])
         lorc.copy_pages(st["pool"], st["copy_src"], st["copy_dst"])
         lorc.reserve_pages(st["block_table"], st["page_refs"], st["gone"], st["lens"], st["status"], workspace=st["workspace"])
         return _moved(st, "page_map")
@@ -325,10 +325,10 @@ def _run_own(st, kind):
                               st["cache_q8"], st["table_q8"])
         return _codes(st)
     if kind == "decode_absorbed":
-        lorc.decode_attention_absorbed_q8(st["desc"], st["q"], st["ctx_len"], st["max_ctx"], st["packed"], st["cache_q8"], st["block_table"],
+        lorc.decode_attention_absorbed_quantized(st["desc"], st["q"], st["ctx_len"], st["max_ctx"], st["packed"], st["cache_q8"], st["block_table"],
                                           out=st["out"], workspace=st["workspace"])
     else:
-        attend = lorc.decode_attention_plain_q8 if kind == "decode_plain" else lorc.decode_attention_q8
+        attend = lorc.decode_attention_plain_quantized if kind == "decode_plain" else lorc.decode_attention_quantized
         attend(st["desc"], st["q"], st["q_pos"], st["ctx_len"], st["max_ctx"], st["packed"], st["cache_q8"], st["block_table"],
                out=st["out"], workspace=st["workspace"])
     return {"out": st["out"]}
@@ -402,7 +402,7 @@ def _plain_turnover(st):
 
 
 def _plain_quantize(st):
-    r, pool = st["r"], st["cache_q8"]
+    r, pool, cache = st["r"], st["cache_q8"], st["cache"].view(torch.bfloat16)
     dev = pool.device
     pos = st["pos_begin"].view(-1, 1).long() + torch.arange(st["max_tokens"], device=dev)
     seq, tok = torch.nonzero(pos < st["pos_end"].view(-1, 1), as_tuple=True)
@@ -413,7 +413,7 @@ def _plain_quantize(st):
     at_v = ((j // 32 * 4 + t // 16) * 64 + j % 32 + 32 * (t % 16 // 8)) * 8 + t % 8 + PAGE * r
     g = torch.arange(_groups(r), device=dev).view(1, -1)
     for at, first in ((at_k, 0), (at_v, _groups(r))):
-        codes, scales = _encode(st["cache"][src, at].float())
+        codes, scales = _encode(cache[src, at].float())
         pool[dst, at] = codes.view(torch.uint8)
         pool[dst, 2 * PAGE * r + (first + g) * PAGE + t] = scales
     return _codes(st)
@@ -485,7 +485,7 @@ def exact(case, seed):
                 new = (pos >= st["pos_begin"][s]) & (pos < st["pos_end"][s])
                 src, dst = int(table[s, page]), int(st["table_q8"][s, page])
                 for part in range(2):
-                    x = st["cache"][src].double()[at[part]]
+                    x = st["cache"][src].view(torch.bfloat16).double()[at[part]]
                     most = torch.cat([x[:, g:g + GROUP].abs().amax(1, keepdim=True).expand(-1, min(GROUP, r - g)) for g in range(0, r, GROUP)], 1)
                     scale = torch.exp2(torch.ceil(torch.log2(most / 448.0)))  # (exact where it matters: bf16 / 448 is no power of two but 448 2^k)
                     y = x / scale
