@@ -283,6 +283,98 @@ int lorc_prefill_attention_plain(const lorc_layer_desc* desc, const void* q, con
                                  const int32_t* block_table, int32_t max_pages, int32_t n_pages, void* out,
                                  void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------------------------- pages
+ * Bookkeeping of the paged cache on the device, for both page formats.  DEVICE pointers.  The state is the caller's:
+ *   block_table [n_seqs x max_pages] int32; an id outside [0, n_pages) maps nothing (these calls write -1)
+ *   page_refs   [n_pages] int32: how many entries map the page; pages whose count is not positive are free
+ * One table and one count array may serve the pools of all layers: the calls that change them return which pages to copy, and
+ * lorc_copy_pages is called once per pool.  Results do not depend on timing: pages are given out by rank.  A call reads its
+ * lists when it runs on the stream; a list of 0 entries is LORC_OK.  status[i] (one per list entry) is one of: */
+#define LORC_PAGES_OK 0
+#define LORC_PAGES_REFUSED 1 /* an index or length out of range, a row that the call cannot take (see there): nothing changed for it */
+#define LORC_PAGES_SHORT 2   /* not enough free pages: nothing changed for it                                                       */
+
+/* Bytes of the workspace (256-byte aligned) that forking and reserving need; 0 for sizes that are not positive. */
+size_t lorc_pages_workspace_bytes(int32_t n_seqs, int32_t n_pages);
+
+/* Pool page src[i] -> pool page dst[i], i < count.  Pairs with an id outside [0, n_pages) (or src[i] = dst[i]) are skipped, so that the
+ * lists of the calls below go in as they are.  No dst may occur twice or be a src of the same call.
+ *   page_bytes  lorc_page_bytes, lorc_page_bytes_quantized, or any multiple of 16; pool: n_pages * page_bytes bytes, 16-byte aligned */
+int lorc_copy_pages(void* pool, size_t page_bytes, int32_t n_pages, const int32_t* src, const int32_t* dst, int32_t count, void* stream);
+
+/* Row children[i] becomes a continuation of the first lens[i] positions of row parents[i], i < n: whole pages are shared, a last page
+ * that is not full becomes a page of the child's own (the lowest free one), which has to be filled from the parent's:
+ *   copy_src, copy_dst [n]  the pair to copy, -1 where there is none
+ * Entries of the parent that map nothing stay unmapped in the child; the rest of the child's row maps nothing.
+ * LORC_PAGES_REFUSED: a row outside the table, lens[i] outside [0, 64 max_pages], parents[i] = children[i], a child whose first entry
+ * maps a page (free it first) or that an earlier pair names, a parent that any pair names as its child.  Pairs are served in order:
+ * once free pages run out, the pairs that need one are LORC_PAGES_SHORT. */
+int lorc_fork_sequences(int32_t* block_table, int32_t n_seqs, int32_t max_pages, int32_t* page_refs, int32_t n_pages,
+                        const int32_t* parents, const int32_t* children, const int32_t* lens, int32_t n, int32_t* copy_src,
+                        int32_t* copy_dst, int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Releases rows seqs[i], i < n: each entry's page loses a count, the entry maps nothing afterwards.  Rows outside the table are
+ * skipped; a row named twice is released once. */
+int lorc_free_sequences(int32_t* block_table, int32_t n_seqs, int32_t max_pages, int32_t* page_refs, int32_t n_pages,
+                        const int32_t* seqs, int32_t n, void* stream);
+
+/* Makes the pool dense: with U pages in use, the k-th lowest free page takes the place of the k-th highest used one while that is
+ * lower, at most max_moves times.  Counts and every entry of the table are renamed; the contents are the caller's to copy:
+ *   move_src, move_dst [max_moves]  pages to copy (lorc_copy_pages takes them), -1 behind the last
+ *   page_map [n_pages]  new id of every page (its own where nothing moved)
+ * Forks of a page (counts above one) move with it.  max_moves = n_pages / 2 always makes the pool dense. */
+int lorc_compact_pages(int32_t* block_table, int32_t n_seqs, int32_t max_pages, int32_t* page_refs, int32_t n_pages,
+                       int32_t* move_src, int32_t* move_dst, int32_t max_moves, int32_t* page_map, void* stream);
+
+/* Gives row seqs[i], i < n, pages for its first lens[i] positions: entries below ceil(lens[i] / 64) that map nothing take the lowest
+ * free pages, in the order of the list and of the row, each with a count of one.  All of a row's or none: LORC_PAGES_SHORT once they
+ * do not all fit (and then for every later row that needs any).  LORC_PAGES_REFUSED: a row outside the table or named before, lens[i]
+ * outside [0, 64 max_pages]. */
+int lorc_reserve_pages(int32_t* block_table, int32_t n_seqs, int32_t max_pages, int32_t* page_refs, int32_t n_pages,
+                       const int32_t* seqs, const int32_t* lens, int32_t n, int32_t* status, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------- 8-bit cache
+ * A pool of pages that hold the latents (of an uncompressed layer: keys and values) as OCP e4m3 codes with a power of two for every
+ * position and 128 consecutive latents (a KV head of an uncompressed layer; the last group may be shorter): half the bytes of a bf16
+ * page + 1/128.  Page p starts at byte p * lorc_page_bytes_quantized().  Code of K latent j of slot t: byte lorc_cache_index_k(t, j), V likewise
+ * (the element order of bf16 pages); behind the 64 (r_k + r_v) codes the scale bytes, [groups of K, then groups of V][64 slots]:
+ *   value = e4m3(code) * 2^(byte - 127);   byte - 127 = the least k >= -126 with (largest finite magnitude of the group) <= 448 * 2^k
+ * A latent that is inf or NaN has a NaN code and does not count in the magnitude.  Tables, tails and page calls are those of bf16 pages. */
+size_t lorc_page_bytes_quantized(const lorc_layer_desc* desc);
+/* Byte inside an 8-bit page of the scale of K (V) latent j of slot t; -1 for an invalid desc or out-of-range argument. */
+int64_t lorc_cache_scale_index_k(const lorc_layer_desc* desc, int32_t slot, int32_t j);
+int64_t lorc_cache_scale_index_v(const lorc_layer_desc* desc, int32_t slot, int32_t j);
+
+/* Positions [pos_begin[s], pos_end[s]) of every sequence s < b from a bf16 pool into an 8-bit pool: a prompt after its prefill, or the
+ * token that lorc_append_latent just wrote (its bf16 page may be one per sequence, reused for every page of positions).  DEVICE pointers.
+ *   cache, block_table [b x max_pages], n_pages           the bf16 pool that is read
+ *   cache_q8, block_table_q8 [b x max_pages_q8], n_pages_q8  the 8-bit pool that is written
+ *   max_tokens  host bound of pos_end - pos_begin, sizes the launch; longer ranges are cut off there, empty ones (end <= begin) do nothing
+ * Positions whose page either table does not map are skipped.  Every other byte of the pool is untouched. */
+int lorc_quantize_latents(const lorc_layer_desc* desc, const void* cache, const int32_t* block_table, int32_t max_pages, int32_t n_pages,
+                          const int32_t* pos_begin, const int32_t* pos_end, int32_t b, int32_t max_tokens, void* cache_q8,
+                          const int32_t* block_table_q8, int32_t max_pages_q8, int32_t n_pages_q8, void* stream);
+
+/* Decode attention over 8-bit pages: arguments, conventions and result of lorc_decode_attention, lorc_decode_attention_plain and
+ * lorc_decode_attention_absorbed on the values that the pages stand for, with cache and n_pages those of the 8-bit pool.
+ *   workspace   lorc_decode_quantized_workspace_bytes (lorc_decode_plain_..., lorc_decode_absorbed_...) bytes, 256-byte aligned, or as many as any call
+ *               with at least this b and max_ctx asks for
+ * rotary: ranks up to 1024;  uncompressed: head_dim 128, rank_k = rank_v = n;  absorbed: ranks up to 1024;  64 query heads each;
+ * otherwise the workspace size is 0 and the call LORC_EUNSUPPORTED. */
+size_t lorc_decode_quantized_workspace_bytes(const lorc_layer_desc* desc, int32_t b, int32_t max_ctx);
+int lorc_decode_attention_quantized(const lorc_layer_desc* desc, const void* q, const int32_t* q_pos, const int32_t* ctx_len, int32_t b,
+                             int32_t max_ctx, const void* packed, const void* cache_q8, const int32_t* block_table, int32_t max_pages,
+                             int32_t n_pages, void* out, void* workspace, size_t workspace_bytes, void* stream);
+size_t lorc_decode_plain_quantized_workspace_bytes(const lorc_layer_desc* desc, int32_t b, int32_t max_ctx);
+int lorc_decode_attention_plain_quantized(const lorc_layer_desc* desc, const void* q, const int32_t* q_pos, const int32_t* ctx_len, int32_t b,
+                                   int32_t max_ctx, const void* packed, const void* cache_q8, const int32_t* block_table,
+                                   int32_t max_pages, int32_t n_pages, void* out, void* workspace, size_t workspace_bytes, void* stream);
+size_t lorc_decode_absorbed_quantized_workspace_bytes(const lorc_layer_desc* desc, int32_t b, int32_t max_ctx);
+int lorc_decode_attention_absorbed_quantized(const lorc_layer_desc* desc, const void* q_lat, const int32_t* ctx_len, int32_t b, int32_t max_ctx,
+                                      const void* packed, const void* cache_q8, const int32_t* block_table, int32_t max_pages,
+                                      int32_t n_pages, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Measurement aid: streams `bytes` (multiple of 16) from src with 16-byte loads and folds them into
  * sink[0] (4 bytes); gives the practical HBM read ceiling that the decode roofline is compared with. */
 int lorc_stream_read_probe(const void* src, size_t bytes, void* sink, void* stream);

@@ -89,6 +89,22 @@ def _load():
         "lorc_prefill_workspace_bytes": (sz, [dsc, i32, i32]),
         "lorc_prefill_attention": (ctypes.c_int, [dsc, vp, vp, i32, i32, i32, vp, vp, vp, i32, i32, vp, vp, sz, vp]),
         "lorc_prefill_attention_plain": (ctypes.c_int, [dsc, vp, vp, i32, i32, i32, vp, vp, vp, i32, i32, vp, vp, sz, vp]),
+        "lorc_pages_workspace_bytes": (sz, [i32, i32]),
+        "lorc_copy_pages": (ctypes.c_int, [vp, sz, i32, vp, vp, i32, vp]),
+        "lorc_fork_sequences": (ctypes.c_int, [vp, i32, i32, vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]),
+        "lorc_free_sequences": (ctypes.c_int, [vp, i32, i32, vp, i32, vp, i32, vp]),
+        "lorc_compact_pages": (ctypes.c_int, [vp, i32, i32, vp, i32, vp, vp, i32, vp, vp]),
+        "lorc_reserve_pages": (ctypes.c_int, [vp, i32, i32, vp, i32, vp, vp, i32, vp, vp, sz, vp]),
+        "lorc_page_bytes_quantized": (sz, [dsc]),
+        "lorc_cache_scale_index_k": (ctypes.c_int64, [dsc, i32, i32]),
+        "lorc_cache_scale_index_v": (ctypes.c_int64, [dsc, i32, i32]),
+        "lorc_quantize_latents": (ctypes.c_int, [dsc, vp, vp, i32, i32, vp, vp, i32, i32, vp, vp, i32, i32, vp]),
+        "lorc_decode_quantized_workspace_bytes": (sz, [dsc, i32, i32]),
+        "lorc_decode_attention_quantized": (ctypes.c_int, [dsc, vp, vp, vp, i32, i32, vp, vp, vp, i32, i32, vp, vp, sz, vp]),
+        "lorc_decode_plain_quantized_workspace_bytes": (sz, [dsc, i32, i32]),
+        "lorc_decode_attention_plain_quantized": (ctypes.c_int, [dsc, vp, vp, vp, i32, i32, vp, vp, vp, i32, i32, vp, vp, sz, vp]),
+        "lorc_decode_absorbed_quantized_workspace_bytes": (sz, [dsc, i32, i32]),
+        "lorc_decode_attention_absorbed_quantized": (ctypes.c_int, [dsc, vp, vp, i32, i32, vp, vp, vp, i32, i32, vp, vp, sz, vp]),
         "lorc_stream_read_probe": (ctypes.c_int, [vp, sz, vp, vp]),
         "lorc_mfma_rate_probe": (ctypes.c_int, [vp, sz, i32, i32, i32, vp]),
     }
@@ -106,7 +122,14 @@ EXPORTS = ("lorc_strerror", "lorc_factorize", "lorc_rank_schedule", "lorc_error_
            "lorc_decode_attention_latent", "lorc_decode_plain_workspace_bytes", "lorc_decode_attention_plain", "lorc_decode_attention_static", "lorc_decode_absorbed_workspace_bytes", "lorc_decode_attention_absorbed",
            "lorc_decode_attention_absorbed_timed",
            "lorc_prefill_workspace_bytes",
-           "lorc_prefill_attention", "lorc_prefill_attention_plain", "lorc_stream_read_probe", "lorc_mfma_rate_probe")
+           "lorc_prefill_attention", "lorc_prefill_attention_plain",
+           "lorc_pages_workspace_bytes", "lorc_copy_pages", "lorc_fork_sequences", "lorc_free_sequences", "lorc_compact_pages",
+           "lorc_reserve_pages",
+           "lorc_page_bytes_quantized", "lorc_cache_scale_index_k", "lorc_cache_scale_index_v", "lorc_quantize_latents",
+           "lorc_decode_quantized_workspace_bytes", "lorc_decode_attention_quantized",
+           "lorc_decode_plain_quantized_workspace_bytes", "lorc_decode_attention_plain_quantized",
+           "lorc_decode_absorbed_quantized_workspace_bytes", "lorc_decode_attention_absorbed_quantized",
+           "lorc_stream_read_probe", "lorc_mfma_rate_probe")
 
 
 def strerror(code: int) -> str:
@@ -434,6 +457,165 @@ def prefill_attention(desc: LayerDesc, q, cu_seqlens, max_seqlen, packed, cache,
     _check(fn(ctypes.byref(desc), _ptr(q), _ptr(cu_seqlens), b, total, max_seqlen, _ptr(packed), _ptr(cache),
               _ptr(block_table), max_pages, n_pages, _ptr(out), _ptr(workspace), workspace.numel(), _stream()), name)
     return out
+
+
+# ---- pages
+PAGES_OK, PAGES_REFUSED, PAGES_SHORT = 0, 1, 2  # status of a list entry
+
+
+def pages_workspace_bytes(n_seqs: int, n_pages: int) -> int:
+    return _lib.lorc_pages_workspace_bytes(n_seqs, n_pages)
+
+
+def _table(block_table, page_refs):
+    _dev(block_table, torch.int32, "block_table")
+    _dev(page_refs, torch.int32, "page_refs")
+    n_seqs, max_pages = block_table.shape
+    return (_ptr(block_table), n_seqs, max_pages, _ptr(page_refs), page_refs.numel())
+
+
+def _lists(n, **lists):
+    for name, t in lists.items():
+        _dev(t, torch.int32, name)
+        assert t.numel() == n, name
+
+
+def _pages_workspace(block_table, page_refs, workspace):
+    if workspace is None:
+        workspace = torch.empty(pages_workspace_bytes(block_table.shape[0], page_refs.numel()), dtype=torch.uint8, device=block_table.device)
+    return _dev(workspace, torch.uint8, "workspace")
+
+
+def copy_pages(pool, src, dst, page_bytes=None):
+    """Pool page src[i] -> dst[i] (see lorc_copy_pages).  pool: any contiguous tensor whose first dimension is the page, or a flat one
+    with the bytes of a page; src, dst int32, pairs with an id outside the pool are skipped."""
+    if not (isinstance(pool, torch.Tensor) and pool.is_cuda and pool.is_contiguous()):
+        raise TypeError("pool: expected a contiguous CUDA tensor")
+    total = pool.numel() * pool.element_size()
+    if page_bytes is None:
+        page_bytes = total // pool.shape[0]
+    _lists(src.numel(), src=src, dst=dst)
+    _check(_lib.lorc_copy_pages(_ptr(pool), page_bytes, total // page_bytes if page_bytes > 0 else 0, _ptr(src), _ptr(dst), src.numel(),
+                                _stream()), "lorc_copy_pages")
+
+
+def fork_sequences(block_table, page_refs, parents, children, lens, copy_src, copy_dst, status, workspace=None):
+    """Rows children[i] continue the first lens[i] positions of rows parents[i] (see lorc_fork_sequences); copy_src, copy_dst, status [n]
+    int32 are written: the pages to copy (copy_pages takes them) and what became of each pair."""
+    n = parents.numel()
+    _lists(n, parents=parents, children=children, lens=lens, copy_src=copy_src, copy_dst=copy_dst, status=status)
+    workspace = _pages_workspace(block_table, page_refs, workspace)
+    _check(_lib.lorc_fork_sequences(*_table(block_table, page_refs), _ptr(parents), _ptr(children), _ptr(lens), n, _ptr(copy_src),
+                                    _ptr(copy_dst), _ptr(status), _ptr(workspace), workspace.numel(), _stream()), "lorc_fork_sequences")
+
+
+def free_sequences(block_table, page_refs, seqs):
+    """Releases the rows (see lorc_free_sequences)."""
+    _dev(seqs, torch.int32, "seqs")
+    _check(_lib.lorc_free_sequences(*_table(block_table, page_refs), _ptr(seqs), seqs.numel(), _stream()), "lorc_free_sequences")
+
+
+def compact_pages(block_table, page_refs, move_src, move_dst, page_map):
+    """Makes the pool dense with at most move_src.numel() moves (see lorc_compact_pages); move_src, move_dst and page_map [n_pages] int32 are
+    written, the pages' contents are the caller's to move (copy_pages)."""
+    _lists(move_src.numel(), move_src=move_src, move_dst=move_dst)
+    _lists(page_refs.numel(), page_map=page_map)
+    _check(_lib.lorc_compact_pages(*_table(block_table, page_refs), _ptr(move_src), _ptr(move_dst), move_src.numel(), _ptr(page_map),
+                                   _stream()), "lorc_compact_pages")
+
+
+def reserve_pages(block_table, page_refs, seqs, lens, status, workspace=None):
+    """Gives rows seqs[i] pages for their first lens[i] positions (see lorc_reserve_pages); status [n] int32 is written."""
+    n = seqs.numel()
+    _lists(n, seqs=seqs, lens=lens, status=status)
+    workspace = _pages_workspace(block_table, page_refs, workspace)
+    _check(_lib.lorc_reserve_pages(*_table(block_table, page_refs), _ptr(seqs), _ptr(lens), n, _ptr(status), _ptr(workspace),
+                                   workspace.numel(), _stream()), "lorc_reserve_pages")
+
+
+# ---- 8-bit cache
+def page_bytes_quantized(desc: LayerDesc) -> int:
+    return _lib.lorc_page_bytes_quantized(ctypes.byref(desc))
+
+
+def cache_scale_index_k(desc: LayerDesc, slot: int, j: int) -> int:
+    return _lib.lorc_cache_scale_index_k(ctypes.byref(desc), slot, j)
+
+
+def cache_scale_index_v(desc: LayerDesc, slot: int, j: int) -> int:
+    return _lib.lorc_cache_scale_index_v(ctypes.byref(desc), slot, j)
+
+
+def quantize_latents(desc: LayerDesc, cache, block_table, pos_begin, pos_end, max_tokens, cache_q8, block_table_q8):
+    """Positions [pos_begin[s], pos_end[s]) of every sequence from the bf16 pool into the 8-bit pool (see lorc_quantize_latents); max_tokens:
+    host bound of their number per sequence."""
+    _dev(cache, torch.uint8, "cache")
+    _dev(cache_q8, torch.uint8, "cache_q8")
+    _dev(block_table, torch.int32, "block_table")
+    _dev(block_table_q8, torch.int32, "block_table_q8")
+    b = pos_begin.numel()
+    _lists(b, pos_begin=pos_begin, pos_end=pos_end)
+    assert block_table.shape[0] >= b and block_table_q8.shape[0] >= b
+    page, page_q8 = page_bytes(desc), page_bytes_quantized(desc)
+    if page == 0:
+        raise LorcError(EUNSUPPORTED, "lorc_page_bytes")
+    _check(_lib.lorc_quantize_latents(ctypes.byref(desc), _ptr(cache), _ptr(block_table), block_table.shape[1], cache.numel() // page,
+                                      _ptr(pos_begin), _ptr(pos_end), b, max_tokens, _ptr(cache_q8), _ptr(block_table_q8),
+                                      block_table_q8.shape[1], cache_q8.numel() // page_q8, _stream()), "lorc_quantize_latents")
+
+
+def decode_quantized_workspace_bytes(desc: LayerDesc, b: int, max_ctx: int) -> int:
+    return _lib.lorc_decode_quantized_workspace_bytes(ctypes.byref(desc), b, max_ctx)
+
+
+def decode_plain_quantized_workspace_bytes(desc: LayerDesc, b: int, max_ctx: int) -> int:
+    return _lib.lorc_decode_plain_quantized_workspace_bytes(ctypes.byref(desc), b, max_ctx)
+
+
+def decode_absorbed_quantized_workspace_bytes(desc: LayerDesc, b: int, max_ctx: int) -> int:
+    return _lib.lorc_decode_absorbed_quantized_workspace_bytes(ctypes.byref(desc), b, max_ctx)
+
+
+def _decode_quantized(name, size, desc, q, width, positions, ctx_len, max_ctx, packed, cache, block_table, out, workspace):
+    _dev(q, torch.bfloat16, "q")
+    for t, nm in ((ctx_len, "ctx_len"), (block_table, "block_table"), *positions):
+        _dev(t, torch.int32, nm)
+    _dev(cache, torch.uint8, "cache")
+    b = q.shape[0]
+    assert tuple(q.shape) == (b, desc.n_q_heads, width) and ctx_len.numel() == b and all(t.numel() == b for t, _ in positions)
+    n_seqs, max_pages = block_table.shape
+    assert n_seqs >= b
+    if workspace is None:
+        workspace = torch.empty(max(size(ctypes.byref(desc), b, max_ctx), 256), dtype=torch.uint8, device=q.device)
+    if out is None:
+        out = torch.empty(b, desc.n_q_heads, desc.head_dim, dtype=torch.bfloat16, device=q.device)
+    page = page_bytes_quantized(desc)
+    if page == 0:
+        raise LorcError(EUNSUPPORTED, "lorc_page_bytes_quantized")
+    _check(getattr(_lib, name)(ctypes.byref(desc), _ptr(q), *(_ptr(t) for t, _ in positions), _ptr(ctx_len), b, max_ctx, _ptr(packed),
+                               _ptr(cache), _ptr(block_table), max_pages, cache.numel() // page, _ptr(out), _ptr(workspace),
+                               workspace.numel(), _stream()), name)
+    return out
+
+
+def decode_attention_quantized(desc: LayerDesc, q, q_pos, ctx_len, max_ctx, packed, cache_q8, block_table, out=None, workspace=None):
+    """decode_attention over an 8-bit pool."""
+    return _decode_quantized("lorc_decode_attention_quantized", _lib.lorc_decode_quantized_workspace_bytes, desc, q, desc.head_dim,
+                             ((q_pos, "q_pos"),), ctx_len, max_ctx, packed, cache_q8, block_table, out, workspace)
+
+
+def decode_attention_plain_quantized(desc: LayerDesc, q, q_pos, ctx_len, max_ctx, packed, cache_q8, block_table, out=None,
+                                     workspace=None):
+    """decode_attention_plain (an uncompressed layer) over an 8-bit pool."""
+    return _decode_quantized("lorc_decode_attention_plain_quantized", _lib.lorc_decode_plain_quantized_workspace_bytes, desc, q,
+                             desc.head_dim, ((q_pos, "q_pos"),), ctx_len, max_ctx, packed, cache_q8, block_table, out, workspace)
+
+
+def decode_attention_absorbed_quantized(desc: LayerDesc, q_lat, ctx_len, max_ctx, packed, cache_q8, block_table, out=None,
+                                        workspace=None):
+    """decode_attention_absorbed (no rotation, key factor folded into the query) over an 8-bit pool."""
+    return _decode_quantized("lorc_decode_attention_absorbed_quantized", _lib.lorc_decode_absorbed_quantized_workspace_bytes, desc, q_lat,
+                             desc.rank_k, (), ctx_len, max_ctx, packed, cache_q8, block_table, out, workspace)
 
 
 def mfma_rate_probe(sink, workgroups: int, iters: int, operands: int = 0):

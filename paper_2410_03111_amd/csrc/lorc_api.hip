@@ -36,6 +36,7 @@ int device_ready(int* n_cus) {
     if (int rc = set_kernel_attributes_append()) return rc;
     if (int rc = set_kernel_attributes_decode()) return rc;
     if (int rc = set_kernel_attributes_prefill()) return rc;
+    if (int rc = set_kernel_attributes_decode_q8()) return rc;
     void* sp = nullptr;
     if (hipGetSymbolAddress(&sp, HIP_SYMBOL(scratch)) != hipSuccess || sp == nullptr) return LORC_EHIP;
     g_scratch_ptr[dev] = sp;
@@ -387,6 +388,192 @@ int lorc_prefill_attention_plain(const lorc_layer_desc* desc, const void* q, con
                                  void* workspace, size_t workspace_bytes, void* stream) {
   return prefill_common(desc, q, cu_seqlens, b, total_tokens, max_seqlen, packed, cache, block_table, max_pages, n_pages, out,
                         workspace, workspace_bytes, stream, true);
+}
+
+// ---- pages
+namespace {
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+int table_args(const void* block_table, int32_t n_seqs, int32_t max_pages, const void* page_refs, int32_t n_pages) {
+  if (!block_table || !page_refs || n_seqs <= 0 || max_pages <= 0 || n_pages <= 0) return LORC_EINVAL;
+  return max_pages > INT32_MAX / kPage ? LORC_EINVAL : LORC_OK;
+}
+}  // namespace
+
+size_t lorc_pages_workspace_bytes(int32_t n_seqs, int32_t n_pages) {
+  if (n_seqs <= 0 || n_pages <= 0) return 0;
+  return 2 * align256((size_t)n_seqs * 4) + align256((size_t)n_pages * 4);
+}
+
+int lorc_copy_pages(void* pool, size_t page_bytes, int32_t n_pages, const int32_t* src, const int32_t* dst, int32_t count, void* stream) {
+  if (!pool || !src || !dst || n_pages <= 0 || count < 0 || page_bytes == 0 || (page_bytes & 15) || !aligned16(pool)) return LORC_EINVAL;
+  if (count == 0) return LORC_OK;
+  return launch_copy_pages(pool, page_bytes, n_pages, src, dst, count, static_cast<hipStream_t>(stream));
+}
+
+int lorc_fork_sequences(int32_t* block_table, int32_t n_seqs, int32_t max_pages, int32_t* page_refs, int32_t n_pages,
+                        const int32_t* parents, const int32_t* children, const int32_t* lens, int32_t n, int32_t* copy_src,
+                        int32_t* copy_dst, int32_t* status, void* workspace, size_t workspace_bytes, void* stream) {
+  if (int rc = table_args(block_table, n_seqs, max_pages, page_refs, n_pages)) return rc;
+  if (!parents || !children || !lens || !copy_src || !copy_dst || !status || !workspace || n < 0) return LORC_EINVAL;
+  if (reinterpret_cast<uintptr_t>(workspace) & 255) return LORC_EINVAL;
+  if (workspace_bytes < lorc_pages_workspace_bytes(n_seqs, n_pages)) return LORC_EWORKSPACE;
+  if (n == 0) return LORC_OK;
+  ForkParams p;
+  p.block_table = block_table;
+  p.page_refs = page_refs;
+  p.parents = parents;
+  p.children = children;
+  p.lens = lens;
+  p.copy_src = copy_src;
+  p.copy_dst = copy_dst;
+  p.status = status;
+  p.owner = static_cast<int32_t*>(workspace);
+  p.asks = reinterpret_cast<int32_t*>(static_cast<unsigned char*>(workspace) + align256((size_t)n_seqs * 4));
+  p.n = n;
+  p.n_seqs = n_seqs;
+  p.max_pages = max_pages;
+  p.n_pages = n_pages;
+  return launch_fork(p, static_cast<hipStream_t>(stream));
+}
+
+int lorc_free_sequences(int32_t* block_table, int32_t n_seqs, int32_t max_pages, int32_t* page_refs, int32_t n_pages,
+                        const int32_t* seqs, int32_t n, void* stream) {
+  if (int rc = table_args(block_table, n_seqs, max_pages, page_refs, n_pages)) return rc;
+  if (!seqs || n < 0) return LORC_EINVAL;
+  if (n == 0) return LORC_OK;
+  return launch_free(block_table, n_seqs, max_pages, page_refs, n_pages, seqs, n, static_cast<hipStream_t>(stream));
+}
+
+int lorc_compact_pages(int32_t* block_table, int32_t n_seqs, int32_t max_pages, int32_t* page_refs, int32_t n_pages,
+                       int32_t* move_src, int32_t* move_dst, int32_t max_moves, int32_t* page_map, void* stream) {
+  if (int rc = table_args(block_table, n_seqs, max_pages, page_refs, n_pages)) return rc;
+  if (!page_map || max_moves < 0 || (max_moves > 0 && (!move_src || !move_dst))) return LORC_EINVAL;
+  CompactParams p;
+  p.block_table = block_table;
+  p.page_refs = page_refs;
+  p.move_src = move_src;
+  p.move_dst = move_dst;
+  p.page_map = page_map;
+  p.max_moves = max_moves;
+  p.n_seqs = n_seqs;
+  p.max_pages = max_pages;
+  p.n_pages = n_pages;
+  return launch_compact(p, static_cast<hipStream_t>(stream));
+}
+
+int lorc_reserve_pages(int32_t* block_table, int32_t n_seqs, int32_t max_pages, int32_t* page_refs, int32_t n_pages,
+                       const int32_t* seqs, const int32_t* lens, int32_t n, int32_t* status, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+  if (int rc = table_args(block_table, n_seqs, max_pages, page_refs, n_pages)) return rc;
+  if (!seqs || !lens || !status || !workspace || n < 0) return LORC_EINVAL;
+  if (reinterpret_cast<uintptr_t>(workspace) & 255) return LORC_EINVAL;
+  if (workspace_bytes < lorc_pages_workspace_bytes(n_seqs, n_pages)) return LORC_EWORKSPACE;
+  if (n == 0) return LORC_OK;
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  ReserveParams p;
+  p.block_table = block_table;
+  p.page_refs = page_refs;
+  p.seqs = seqs;
+  p.lens = lens;
+  p.status = status;
+  p.owner = reinterpret_cast<int32_t*>(ws);
+  p.first = reinterpret_cast<int32_t*>(ws + align256((size_t)n_seqs * 4));
+  p.pages = reinterpret_cast<int32_t*>(ws + 2 * align256((size_t)n_seqs * 4));
+  p.n = n;
+  p.n_seqs = n_seqs;
+  p.max_pages = max_pages;
+  p.n_pages = n_pages;
+  return launch_reserve(p, static_cast<hipStream_t>(stream));
+}
+
+// ---- 8-bit cache
+int lorc_quantize_latents(const lorc_layer_desc* desc, const void* cache, const int32_t* block_table, int32_t max_pages, int32_t n_pages,
+                          const int32_t* pos_begin, const int32_t* pos_end, int32_t b, int32_t max_tokens, void* cache_q8,
+                          const int32_t* block_table_q8, int32_t max_pages_q8, int32_t n_pages_q8, void* stream) {
+  if (!desc || !cache || !block_table || !pos_begin || !pos_end || !cache_q8 || !block_table_q8) return LORC_EINVAL;
+  if (int rc = check_desc(*desc)) return rc;
+  if (b <= 0 || max_tokens < 0 || max_pages <= 0 || n_pages <= 0 || max_pages_q8 <= 0 || n_pages_q8 <= 0) return LORC_EINVAL;
+  if (!aligned16(cache) || !aligned16(cache_q8)) return LORC_EINVAL;
+  if (max_tokens == 0) return LORC_OK;
+  QuantizeParams p;
+  p.src = static_cast<const uint16_t*>(cache);
+  p.dst = static_cast<unsigned char*>(cache_q8);
+  p.src_table = block_table;
+  p.dst_table = block_table_q8;
+  p.pos_begin = pos_begin;
+  p.pos_end = pos_end;
+  p.b = b;
+  p.src_max_pages = max_pages;
+  p.src_pages = n_pages;
+  p.dst_max_pages = max_pages_q8;
+  p.dst_pages = n_pages_q8;
+  const int least = max_pages < max_pages_q8 ? max_pages : max_pages_q8;
+  p.max_tokens = max_tokens;
+  p.span = (int)(((long)max_tokens + 2 * kPage - 2) / kPage);  // pages that max_tokens positions touch at most
+  if (p.span > least) p.span = least;
+  p.r_k = desc->rank_k;
+  p.r_v = desc->rank_v;
+  return launch_quantize(p, static_cast<hipStream_t>(stream));
+}
+
+namespace {
+size_t q8_workspace(const lorc_layer_desc* desc, Q8Form form, int32_t b, int32_t max_ctx) {
+  if (!desc || check_desc(*desc) != LORC_OK || b <= 0 || max_ctx < 0) return 0;
+  return make_q8_plan(*desc, form, b, max_ctx, cu_count_or_default(), kAnySplits).total_bytes;
+}
+
+int decode_q8(const lorc_layer_desc* desc, Q8Form form, const void* q, const int32_t* q_pos, const int32_t* ctx_len, int32_t b,
+              int32_t max_ctx, const void* packed, const void* cache, const int32_t* block_table, int32_t max_pages, int32_t n_pages,
+              void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  const bool rotary = form != Q8Form::kAbsorbed;
+  if (int rc = decode_args(desc, q, q_pos, rotary, ctx_len, b, max_ctx, packed, cache, block_table, max_pages, n_pages, out, workspace))
+    return rc;
+  if (!q8_shape_ok(*desc, form)) return LORC_EUNSUPPORTED;
+  int n_cus = 0;
+  if (int rc = device_ready(&n_cus)) return rc;
+  const DecodePlan plan = make_q8_plan_within(*desc, form, b, max_ctx, n_cus, workspace_bytes);
+  DecodeParams p;
+  if (int rc = decode_params(p, desc, q, q_pos, rotary, ctx_len, b, max_ctx, packed, cache, block_table, max_pages, n_pages, out,
+                             workspace, workspace_bytes, plan, 0, n_cus))
+    return rc;
+  p.page_elems = q8_page_bytes(desc->rank_k, desc->rank_v) / 2;
+  return launch_decode_q8(*desc, form, p, plan, static_cast<hipStream_t>(stream));
+}
+}  // namespace
+
+size_t lorc_decode_quantized_workspace_bytes(const lorc_layer_desc* desc, int32_t b, int32_t max_ctx) {
+  return q8_workspace(desc, Q8Form::kRotary, b, max_ctx);
+}
+
+int lorc_decode_attention_quantized(const lorc_layer_desc* desc, const void* q, const int32_t* q_pos, const int32_t* ctx_len, int32_t b,
+                                    int32_t max_ctx, const void* packed, const void* cache_q8, const int32_t* block_table,
+                                    int32_t max_pages, int32_t n_pages, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  return decode_q8(desc, Q8Form::kRotary, q, q_pos, ctx_len, b, max_ctx, packed, cache_q8, block_table, max_pages, n_pages, out, workspace,
+                   workspace_bytes, stream);
+}
+
+size_t lorc_decode_plain_quantized_workspace_bytes(const lorc_layer_desc* desc, int32_t b, int32_t max_ctx) {
+  return q8_workspace(desc, Q8Form::kPlain, b, max_ctx);
+}
+
+int lorc_decode_attention_plain_quantized(const lorc_layer_desc* desc, const void* q, const int32_t* q_pos, const int32_t* ctx_len,
+                                          int32_t b, int32_t max_ctx, const void* packed, const void* cache_q8, const int32_t* block_table,
+                                          int32_t max_pages, int32_t n_pages, void* out, void* workspace, size_t workspace_bytes,
+                                          void* stream) {
+  return decode_q8(desc, Q8Form::kPlain, q, q_pos, ctx_len, b, max_ctx, packed, cache_q8, block_table, max_pages, n_pages, out, workspace,
+                   workspace_bytes, stream);
+}
+
+size_t lorc_decode_absorbed_quantized_workspace_bytes(const lorc_layer_desc* desc, int32_t b, int32_t max_ctx) {
+  return q8_workspace(desc, Q8Form::kAbsorbed, b, max_ctx);
+}
+
+int lorc_decode_attention_absorbed_quantized(const lorc_layer_desc* desc, const void* q_lat, const int32_t* ctx_len, int32_t b,
+                                             int32_t max_ctx, const void* packed, const void* cache_q8, const int32_t* block_table,
+                                             int32_t max_pages, int32_t n_pages, void* out, void* workspace, size_t workspace_bytes,
+                                             void* stream) {
+  return decode_q8(desc, Q8Form::kAbsorbed, q_lat, nullptr, ctx_len, b, max_ctx, packed, cache_q8, block_table, max_pages, n_pages, out,
+                   workspace, workspace_bytes, stream);
 }
 
 int lorc_stream_read_probe(const void* src, size_t bytes, void* sink, void* stream) {

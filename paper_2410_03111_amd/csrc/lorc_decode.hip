@@ -1362,6 +1362,14 @@ static int launch_merge(const DecodeParams& p, hipStream_t s) {
   return p.head_dim == 128 ? launch_merge_group<128>(p, s) : launch_merge_group<64>(p, s);
 }
 
+int launch_decode_merge(const DecodeParams& p, bool plain, hipStream_t s) {
+  if (!plain) return launch_merge(p, s);
+  DecodeParams pm = p;
+  pm.r_v = p.head_dim;
+  pm.latent_out = 1;
+  return launch_kernel(decode_merge_kernel<128>, dim3(pm.b * pm.h_q), dim3(256), 0, s, pm);
+}
+
 DecodePlan make_absorbed_plan(const lorc_layer_desc& d, int b, int max_ctx, int n_cus, int max_splits) {
   if (d.n_q_heads > 32 || d.rank_k > kAbsMaxRankK || d.rank_v > 512) {
     // beyond the single-pass kernel (one register ring per wave): scores, values in column chunks, merge
@@ -1448,13 +1456,7 @@ int launch_decode(const DecodeParams& p, const DecodePlan& plan, hipStream_t s, 
     if (int rc2 = record(ev_end, s)) return rc2;
     // the generic merge: softmax-merge of the splits; wide layers then apply B_v, uncompressed layers have none
     // (their partial rows are head_dim wide and are written out as they are)
-    if (plan.wide == 2) {
-      DecodeParams pm = p;
-      pm.r_v = p.head_dim;
-      pm.latent_out = 1;
-      return launch_kernel(decode_merge_kernel<128>, dim3(pm.b * pm.h_q), dim3(256), 0, s, pm);
-    }
-    return launch_merge(p, s);  // the group merge where its limits hold, the generic one otherwise
+    return launch_decode_merge(p, plan.wide == 2, s);  // the group merge where its limits hold, the generic one otherwise
   }
   if (plan.stationary == 2) rc = launch_decode_stationary768_split(p, plan, s);
   else if (plan.stationary) rc = launch_decode_stationary_split(p, plan, s);

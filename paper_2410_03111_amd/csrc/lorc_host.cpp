@@ -463,4 +463,18 @@ int64_t lorc_cache_index_v(const lorc_layer_desc* desc, int32_t slot, int32_t j)
   return lorc::v_index(desc->rank_k, slot, j);
 }
 
+size_t lorc_page_bytes_quantized(const lorc_layer_desc* desc) {
+  return desc_ok(desc) ? lorc::q8_page_bytes(desc->rank_k, desc->rank_v) : 0;
+}
+
+int64_t lorc_cache_scale_index_k(const lorc_layer_desc* desc, int32_t slot, int32_t j) {
+  if (!desc_ok(desc) || slot < 0 || slot >= LORC_PAGE_TOKENS || j < 0 || j >= desc->rank_k) return -1;
+  return lorc::q8_scale_k(desc->rank_k, desc->rank_v, slot, j);
+}
+
+int64_t lorc_cache_scale_index_v(const lorc_layer_desc* desc, int32_t slot, int32_t j) {
+  if (!desc_ok(desc) || slot < 0 || slot >= LORC_PAGE_TOKENS || j < 0 || j >= desc->rank_v) return -1;
+  return lorc::q8_scale_v(desc->rank_k, desc->rank_v, slot, j);
+}
+
 }  // extern "C"

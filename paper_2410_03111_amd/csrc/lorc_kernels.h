@@ -103,6 +103,39 @@ struct PrefillParams {
   float rope_base, q_scale;
 };
 
+struct ForkParams {
+  int32_t* block_table;
+  int32_t* page_refs;
+  const int32_t *parents, *children, *lens;
+  int32_t *copy_src, *copy_dst, *status;
+  int32_t *owner, *asks;  // workspace
+  int n, n_seqs, max_pages, n_pages;
+};
+
+struct CompactParams {
+  int32_t* block_table;
+  int32_t* page_refs;
+  int32_t *move_src, *move_dst, *page_map;
+  int max_moves, n_seqs, max_pages, n_pages;
+};
+
+struct ReserveParams {
+  int32_t* block_table;
+  int32_t* page_refs;
+  const int32_t *seqs, *lens;
+  int32_t* status;
+  int32_t *owner, *first, *pages;  // workspace
+  int n, n_seqs, max_pages, n_pages;
+};
+
+struct QuantizeParams {
+  const uint16_t* src;
+  unsigned char* dst;
+  const int32_t *src_table, *dst_table, *pos_begin, *pos_end;
+  int b, max_tokens, span;  // span: pages that max_tokens positions can touch
+  int r_k, r_v, src_max_pages, src_pages, dst_max_pages, dst_pages;
+};
+
 constexpr int kAnySplits = 1 << 20;  // no limit of a plan's splits
 
 // Every launcher returns LORC_OK or the lorc_status of the first launch (or event record) that failed.
@@ -136,6 +169,23 @@ DecodePlan make_absorbed_plan_within(const lorc_layer_desc& d, int b, int max_ct
 int launch_decode_absorbed(const DecodeParams& p, const DecodePlan& plan, hipStream_t s, hipEvent_t ev_begin, hipEvent_t ev_end);
 int launch_stream_probe(const void* src, size_t bytes, void* sink, hipStream_t s);
 int launch_mfma_probe(float* sink, int workgroups, int iters, int operands, hipStream_t s);
+
+int launch_copy_pages(void* pool, size_t page_bytes, int n_pages, const int32_t* src, const int32_t* dst, int count, hipStream_t s);
+int launch_fork(const ForkParams& p, hipStream_t s);
+int launch_free(int32_t* block_table, int n_seqs, int max_pages, int32_t* page_refs, int n_pages, const int32_t* seqs, int n, hipStream_t s);
+int launch_compact(const CompactParams& p, hipStream_t s);
+int launch_reserve(const ReserveParams& p, hipStream_t s);
+int launch_quantize(const QuantizeParams& p, hipStream_t s);
+
+// Decode over 8-bit pages (lorc_decode_q8.hip).  DecodeParams: cache and page_elems are those of the 8-bit pool (page_elems in units of two bytes).
+enum class Q8Form { kRotary, kPlain, kAbsorbed };
+bool q8_shape_ok(const lorc_layer_desc& d, Q8Form form);
+DecodePlan make_q8_plan(const lorc_layer_desc& d, Q8Form form, int b, int max_ctx, int n_cus, int max_splits);
+DecodePlan make_q8_plan_within(const lorc_layer_desc& d, Q8Form form, int b, int max_ctx, int n_cus, size_t bytes);
+int launch_decode_q8(const lorc_layer_desc& d, Q8Form form, const DecodeParams& p, const DecodePlan& plan, hipStream_t s);
+int set_kernel_attributes_decode_q8();
+// The merge that follows a split kernel; plain: partial rows of head_dim coordinates that no factor is applied to.
+int launch_decode_merge(const DecodeParams& p, bool plain, hipStream_t s);
 
 // Kernels that use more than 64 KiB of LDS need a function attribute, set once per device (the call is not
 // capturable into a HIP graph).  Each translation unit sets it for its own kernels.

@@ -51,6 +51,17 @@ LORC_HD int64_t v_index(int r_k, int slot, int j) {
          ((int64_t)((j >> 5) * 4 + (slot >> 4)) * 64 + (j & 31) + 32 * ((slot & 15) >> 3)) * 8 + (slot & 7);
 }
 
+// ---- 8-bit latent cache page: [codes of the K part][codes of the V part][scale bytes], one byte per latent in the element order above.
+// 128 consecutive latents of a position (a KV head of an uncompressed layer; the last group may be shorter) share a power of two;
+// its byte is the exponent + 127, [K groups, then V groups][64 slots].
+constexpr int kQ8Group = 128;
+LORC_HD int q8_groups(int r) { return (r + kQ8Group - 1) / kQ8Group; }
+LORC_HD size_t q8_page_bytes(int r_k, int r_v) { return (size_t)kPage * (size_t)(r_k + r_v + q8_groups(r_k) + q8_groups(r_v)); }
+LORC_HD int64_t q8_scale_k(int r_k, int r_v, int slot, int j) { return (int64_t)kPage * (r_k + r_v + j / kQ8Group) + slot; }
+LORC_HD int64_t q8_scale_v(int r_k, int r_v, int slot, int j) {
+  return (int64_t)kPage * (r_k + r_v + q8_groups(r_k) + j / kQ8Group) + slot;
+}
+
 // ---- packed factors: [At: (r_k + r_v) x D][Bk tiles][Bv tiles][At tiles][rotation tables], element = bf16 ----
 // At row j (< r_k: column j of A_k, else column j - r_k of A_v) is contiguous over the model dimension.
 // B tiles are [c/32][j/16][64 lanes][8]: lane = c%32 + 32*((j%16)/8) holds 8 consecutive latent indices of

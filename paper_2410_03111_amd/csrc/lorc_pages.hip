@@ -1,0 +1,357 @@
+// Bookkeeping of the paged cache on the device: giving out, sharing, releasing and renaming pages, and copying their contents.
+// The state is the caller's block table (an id outside [0, n_pages) maps nothing) and one count per page of the entries that
+// map it.  Everything here is integers: results do not depend on the order in which workgroups or atomics run, because pages
+// are given out by rank (the k-th request takes the k-th lowest free page) and counts only ever see sums.
+//
+// What bounds these calls is the chain of launches and of trips to memory, not the bytes: so each is a plan (one workgroup of
+// 1024 threads that walks the counts 16 to a thread and ranks by a scan over the workgroup) followed, where rows of the table
+// change, by one wave per row.  A plan in several workgroups would need another launch for every scan, 2 to 3 us each, which is
+// what one workgroup takes for the counts of 16384 pages.
+#include <climits>
+
+#include "lorc_device.h"
+#include "lorc_kernels.h"
+
+namespace lorc {
+
+namespace {
+constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64, kPerThread = 16;
+
+__device__ __forceinline__ bool maps(int id, int n_pages) { return id >= 0 && id < n_pages; }
+// Values that other waves of the workgroup wrote through atomics are read past the vector cache.
+__device__ __forceinline__ int load_fresh(const int* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ void store_fresh(int* p, int v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+__device__ __forceinline__ int wave_inclusive(int v) {
+#pragma unroll
+  for (int step = 1; step < 64; step <<= 1) {
+    const int up = __shfl_up(v, step, 64);
+    if ((int)(threadIdx.x & 63) >= step) v += up;
+  }
+  return v;
+}
+
+// Exclusive prefix sum over the workgroup's threads; *total: the sum.  `sums`: kPlanWaves words of LDS.
+__device__ __forceinline__ int block_exclusive(int v, int* sums, int* total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int inc = wave_inclusive(v);
+  __syncthreads();  // the words may still be read from the call before
+  if (lane == 63) sums[w] = inc;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int i = 0; i < kPlanWaves; ++i) {
+    const int s = sums[i];
+    before += i < w ? s : 0;
+    all += s;
+  }
+  *total = all;
+  return before + inc - v;
+}
+
+// The counts of up to 16 consecutive pages from `first` on, as a mask of those that are free (bit set) and how many are there.
+__device__ __forceinline__ uint32_t free_mask(const int* refs, int first, int n_pages) {
+  uint32_t mask = 0;
+  if (first + kPerThread <= n_pages && (reinterpret_cast<uintptr_t>(refs) & 15) == 0) {
+#pragma unroll
+    for (int u = 0; u < kPerThread / 4; ++u) {
+      const int4 v = *reinterpret_cast<const int4*>(refs + first + 4 * u);
+      mask |= (v.x <= 0 ? 1u : 0u) << (4 * u) | (v.y <= 0 ? 2u : 0u) << (4 * u) | (v.z <= 0 ? 4u : 0u) << (4 * u) | (v.w <= 0 ? 8u : 0u) << (4 * u);
+    }
+  } else {
+    for (int u = 0; u < kPerThread; ++u)
+      if (first + u < n_pages && refs[first + u] <= 0) mask |= 1u << u;
+  }
+  return mask;
+}
+
+// emit(k, page) for the free pages of rank k < want, in ascending order; returns how many free pages there are among those walked
+// (all of them where fewer than `want` exist).
+template <typename F>
+__device__ __forceinline__ int each_free(const int* refs, int n_pages, int want, int* sums, F emit) {
+  int seen = 0;
+  for (int base = 0; base < n_pages && seen < want; base += kPlanThreads * kPerThread) {
+    const int first = base + (int)threadIdx.x * kPerThread;
+    uint32_t mask = first < n_pages ? free_mask(refs, first, n_pages) : 0u;
+    int total;
+    int rank = seen + block_exclusive(__popc(mask), sums, &total);
+    while (mask != 0 && rank < want) {
+      emit(rank++, first + __ffs(mask) - 1);
+      mask &= mask - 1;
+    }
+    seen += total;
+  }
+  return seen;
+}
+}  // namespace
+
+// ------------------------------------------------------------------------------------------------ copy
+// One workgroup per 16 KiB piece of a page: 64 bytes per thread in flight.  Bound by memory: every byte is read and written once.
+constexpr int kCopyBytes = 16 * 1024;
+__global__ __launch_bounds__(256) void copy_pages_kernel(unsigned char* pool, size_t page_bytes, int n_pages, const int* __restrict__ src,
+                                                         const int* __restrict__ dst, int pieces) {
+  const int i = blockIdx.x / pieces, piece = blockIdx.x % pieces;
+  const int from = __builtin_amdgcn_readfirstlane(src[i]), to = __builtin_amdgcn_readfirstlane(dst[i]);
+  if (!maps(from, n_pages) || !maps(to, n_pages) || from == to) return;
+  const size_t at = (size_t)piece * kCopyBytes;
+  const int n16 = (int)((page_bytes - at < kCopyBytes ? page_bytes - at : kCopyBytes) >> 4);
+  const u32x4* s = reinterpret_cast<const u32x4*>(pool + (size_t)from * page_bytes + at);
+  u32x4* d = reinterpret_cast<u32x4*>(pool + (size_t)to * page_bytes + at);
+  u32x4 v[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int k = (int)threadIdx.x + 256 * u;
+    if (k < n16) v[u] = s[k];
+  }
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int k = (int)threadIdx.x + 256 * u;
+    if (k < n16) d[k] = v[u];
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ fork
+// Workspace: owner [n_seqs] (the lowest pair that names a row as its child), asks [n_seqs] (pairs that need a page, in order).
+__global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(ForkParams p) {
+  __shared__ int sums[kPlanWaves];
+  const int tid = threadIdx.x;
+  for (int s = tid; s < p.n_seqs; s += kPlanThreads) store_fresh(p.owner + s, INT_MAX);
+  __syncthreads();
+  const long most = (long)p.max_pages * kPage;
+  auto named = [&](int i, int& parent, int& child, int& len) {
+    parent = p.parents[i];
+    child = p.children[i];
+    len = p.lens[i];
+    return parent >= 0 && parent < p.n_seqs && child >= 0 && child < p.n_seqs && parent != child && len >= 0 && len <= most;
+  };
+  for (int i = tid; i < p.n; i += kPlanThreads) {
+    int parent, child, len;
+    if (named(i, parent, child, len)) atomicMin(p.owner + child, i);
+  }
+  __syncthreads();
+  int asked = 0;
+  for (int base = 0; base < p.n; base += kPlanThreads) {
+    const int i = base + tid;
+    int parent, child, len, tail = -1;
+    bool ok = i < p.n && named(i, parent, child, len);
+    ok = ok && load_fresh(p.owner + child) == i && load_fresh(p.owner + parent) == INT_MAX &&
+         !maps(p.block_table[(size_t)child * p.max_pages], p.n_pages);
+    if (ok && len % kPage != 0) tail = p.block_table[(size_t)parent * p.max_pages + len / kPage];
+    const bool asks = maps(tail, p.n_pages);
+    int total;
+    const int rank = asked + block_exclusive(asks ? 1 : 0, sums, &total);
+    asked += total;
+    if (asks) store_fresh(p.asks + rank, i);
+    if (i < p.n) {
+      p.status[i] = !ok ? LORC_PAGES_REFUSED : asks ? LORC_PAGES_SHORT : LORC_PAGES_OK;  // (short until a page is found below)
+      p.copy_src[i] = asks ? tail : -1;
+      p.copy_dst[i] = -1;
+    }
+  }
+  __syncthreads();
+  const int found = each_free(p.page_refs, p.n_pages, asked, sums, [&](int k, int page) {
+    const int i = load_fresh(p.asks + k);
+    p.copy_dst[i] = page;
+    p.status[i] = LORC_PAGES_OK;
+  });
+  for (int k = found + tid; k < asked; k += kPlanThreads) p.copy_src[load_fresh(p.asks + k)] = -1;
+}
+
+// One wave per pair: the child's row, and the counts of the pages that it shares.
+__global__ __launch_bounds__(256) void fork_rows_kernel(ForkParams p) {
+  const int i = blockIdx.x * 4 + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (i >= p.n || p.status[i] != LORC_PAGES_OK) return;
+  const int whole = p.lens[i] / kPage, fresh = p.copy_dst[i];
+  const int* from = p.block_table + (size_t)p.parents[i] * p.max_pages;
+  int* to = p.block_table + (size_t)p.children[i] * p.max_pages;
+  for (int e = lane; e < p.max_pages; e += 64) {
+    int id = e < whole ? from[e] : e == whole ? fresh : -1;
+    if (!maps(id, p.n_pages)) id = -1;
+    else if (e < whole) atomicAdd(p.page_refs + id, 1);
+    else p.page_refs[id] = 1;
+    to[e] = id;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ free
+// One wave per row.  An entry is claimed by an exchange, so that a row named twice is released once.
+__global__ __launch_bounds__(256) void free_rows_kernel(int* block_table, int n_seqs, int max_pages, int* page_refs, int n_pages,
+                                                        const int* __restrict__ seqs, int n) {
+  const int i = blockIdx.x * 4 + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (i >= n) return;
+  const int s = seqs[i];
+  if (s < 0 || s >= n_seqs) return;
+  int* row = block_table + (size_t)s * max_pages;
+  for (int e = lane; e < max_pages; e += 64) {
+    const int id = atomicExch(row + e, -1);
+    if (maps(id, n_pages)) atomicSub(page_refs + id, 1);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ compact
+// U pages are in use: the k-th lowest free page (below U) takes the contents of the k-th highest used one (at U or above).
+__global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(CompactParams p) {
+  __shared__ int sums[kPlanWaves];
+  const int tid = threadIdx.x;
+  constexpr int kStep = kPlanThreads * kPerThread;
+  int n_free = 0;
+  for (int base = 0; base < p.n_pages; base += kStep) {
+    const int first = base + tid * kPerThread;
+    int total;
+    block_exclusive(first < p.n_pages ? __popc(free_mask(p.page_refs, first, p.n_pages)) : 0, sums, &total);
+    n_free += total;
+  }
+  const int used = p.n_pages - n_free;
+  int holes = 0;  // free pages below `used`: as many as used pages from there on
+  for (int base = 0; base < used; base += kStep) {
+    const int first = base + tid * kPerThread;
+    uint32_t mask = first < used ? free_mask(p.page_refs, first, p.n_pages) : 0u;
+    if (first < used && first + kPerThread > used) mask &= (1u << (used - first)) - 1u;
+    int total;
+    int rank = holes + block_exclusive(__popc(mask), sums, &total);
+    for (uint32_t m = mask; m != 0; m &= m - 1, ++rank)
+      if (rank < p.max_moves) store_fresh(p.move_dst + rank, first + __ffs(m) - 1);
+    holes += total;
+  }
+  const int moves = holes < p.max_moves ? holes : p.max_moves;
+  __syncthreads();
+  for (int k = moves + tid; k < p.max_moves; k += kPlanThreads) p.move_src[k] = p.move_dst[k] = -1;
+  for (int id = tid; id < used; id += kPlanThreads) p.page_map[id] = id;
+  int rest = holes;  // used pages not yet walked
+  for (int base = used; base < p.n_pages; base += kStep) {
+    const int first = base + tid * kPerThread;
+    int n_here = p.n_pages - first;
+    n_here = n_here < 0 ? 0 : (n_here > kPerThread ? kPerThread : n_here);
+    const uint32_t all = (1u << n_here) - 1u;
+    uint32_t free_here = 0;
+    for (int u = 0; u < n_here; ++u) free_here |= (p.page_refs[first + u] <= 0 ? 1u : 0u) << u;
+    const uint32_t mask = all & ~free_here;
+    int total;
+    int k = rest - 1 - block_exclusive(__popc(mask), sums, &total);  // rank from the top
+    for (int u = 0; u < n_here; ++u) {
+      int to = first + u;
+      if (mask >> u & 1u) {
+        if (k < moves) {
+          to = load_fresh(p.move_dst + k);
+          p.move_src[k] = first + u;
+          p.page_refs[to] = p.page_refs[first + u];
+          p.page_refs[first + u] = 0;
+        }
+        --k;
+      }
+      p.page_map[first + u] = to;
+    }
+    rest -= total;
+  }
+}
+
+__global__ __launch_bounds__(256) void rename_pages_kernel(int* block_table, size_t entries, const int* __restrict__ page_map, int n_pages) {
+  const size_t e = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (e >= entries) return;
+  const int id = block_table[e];
+  if (!maps(id, n_pages)) return;
+  const int to = page_map[id];
+  if (to != id) block_table[e] = to;
+}
+
+// ------------------------------------------------------------------------------------------------ reserve
+// Workspace: owner [n_seqs] (the first place in the list that names a row), first [n_seqs] (rank of the row's first new page),
+// pages [n_pages] (free pages by rank).
+__global__ __launch_bounds__(kPlanThreads) void reserve_plan_kernel(ReserveParams p) {
+  __shared__ int sums[kPlanWaves];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  for (int s = tid; s < p.n_seqs; s += kPlanThreads) store_fresh(p.owner + s, INT_MAX);
+  __syncthreads();
+  const long most = (long)p.max_pages * kPage;
+  auto named = [&](int i, int& s, int& len) {
+    s = p.seqs[i];
+    len = p.lens[i];
+    return s >= 0 && s < p.n_seqs && len >= 0 && len <= most;
+  };
+  for (int i = tid; i < p.n; i += kPlanThreads) {
+    int s, len;
+    if (named(i, s, len)) atomicMin(p.owner + s, i);
+  }
+  __syncthreads();
+  for (int i = w; i < p.n; i += kPlanWaves) {  // how many entries of the row map nothing yet
+    int s, len;
+    if (!named(i, s, len) || load_fresh(p.owner + s) != i) continue;
+    const int n_e = (len + kPage - 1) / kPage;
+    const int* row = p.block_table + (size_t)s * p.max_pages;
+    int missing = 0;
+    for (int e = lane; e < n_e; e += 64) missing += maps(row[e], p.n_pages) ? 0 : 1;
+    missing = wave_inclusive(missing);
+    if (lane == 63) store_fresh(p.first + s, missing);
+  }
+  __syncthreads();
+  int asked = 0;
+  for (int base = 0; base < p.n; base += kPlanThreads) {
+    const int i = base + tid;
+    int s, len;
+    const bool ok = i < p.n && named(i, s, len) && load_fresh(p.owner + s) == i;
+    const int missing = ok ? load_fresh(p.first + s) : 0;
+    int total;
+    const int rank = asked + block_exclusive(missing, sums, &total);
+    asked += total;
+    if (ok) store_fresh(p.first + s, rank);
+    if (i < p.n) p.status[i] = !ok ? LORC_PAGES_REFUSED : missing;  // (the count, until it is known whether they are there)
+  }
+  __syncthreads();
+  const int found = each_free(p.page_refs, p.n_pages, asked, sums, [&](int k, int page) { p.pages[k] = page; });
+  for (int i = tid; i < p.n; i += kPlanThreads) {
+    int s, len;
+    if (!named(i, s, len) || load_fresh(p.owner + s) != i) continue;
+    const int missing = p.status[i];
+    p.status[i] = missing == 0 || load_fresh(p.first + s) + missing <= found ? LORC_PAGES_OK : LORC_PAGES_SHORT;
+  }
+}
+
+__global__ __launch_bounds__(256) void reserve_rows_kernel(ReserveParams p) {
+  const int i = blockIdx.x * 4 + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (i >= p.n || p.status[i] != LORC_PAGES_OK) return;
+  const int s = p.seqs[i], n_e = (p.lens[i] + kPage - 1) / kPage;
+  int* row = p.block_table + (size_t)s * p.max_pages;
+  int rank = p.first[s];
+  for (int e0 = 0; e0 < n_e; e0 += 64) {
+    const int e = e0 + lane;
+    const bool missing = e < n_e && !maps(row[e], p.n_pages);
+    const uint64_t who = __ballot(missing);
+    if (missing) {
+      const int id = p.pages[rank + __popcll(who & ((1ull << lane) - 1ull))];
+      row[e] = id;
+      p.page_refs[id] = 1;
+    }
+    rank += __popcll(who);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ host
+int launch_copy_pages(void* pool, size_t page_bytes, int n_pages, const int32_t* src, const int32_t* dst, int count, hipStream_t s) {
+  const size_t pieces = (page_bytes + kCopyBytes - 1) / kCopyBytes;
+  if (pieces * (size_t)count > 0x7fffffffu) return LORC_EINVAL;
+  return launch_kernel(copy_pages_kernel, dim3((uint32_t)(pieces * count)), dim3(256), 0, s, static_cast<unsigned char*>(pool), page_bytes,
+                       n_pages, src, dst, (int)pieces);
+}
+
+int launch_fork(const ForkParams& p, hipStream_t s) {
+  if (int rc = launch_kernel(fork_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, p)) return rc;
+  return launch_kernel(fork_rows_kernel, dim3((p.n + 3) / 4), dim3(256), 0, s, p);
+}
+
+int launch_free(int32_t* block_table, int n_seqs, int max_pages, int32_t* page_refs, int n_pages, const int32_t* seqs, int n, hipStream_t s) {
+  return launch_kernel(free_rows_kernel, dim3((n + 3) / 4), dim3(256), 0, s, block_table, n_seqs, max_pages, page_refs, n_pages, seqs, n);
+}
+
+int launch_compact(const CompactParams& p, hipStream_t s) {
+  if (int rc = launch_kernel(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, p)) return rc;
+  const size_t entries = (size_t)p.n_seqs * p.max_pages;
+  if (entries > (size_t)0x7fffffff * 256) return LORC_EINVAL;
+  return launch_kernel(rename_pages_kernel, dim3((uint32_t)((entries + 255) / 256)), dim3(256), 0, s, p.block_table, entries, p.page_map, p.n_pages);
+}
+
+int launch_reserve(const ReserveParams& p, hipStream_t s) {
+  if (int rc = launch_kernel(reserve_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, p)) return rc;
+  return launch_kernel(reserve_rows_kernel, dim3((p.n + 3) / 4), dim3(256), 0, s, p);
+}
+
+}  // namespace lorc
