@@ -37,6 +37,7 @@ int device_ready(int* n_cus) {
     if (int rc = set_kernel_attributes_decode()) return rc;
     if (int rc = set_kernel_attributes_prefill()) return rc;
     if (int rc = set_kernel_attributes_decode_q8()) return rc;
+    if (int rc = set_kernel_attributes_decode_q8_stationary()) return rc;
     void* sp = nullptr;
     if (hipGetSymbolAddress(&sp, HIP_SYMBOL(scratch)) != hipSuccess || sp == nullptr) return LORC_EHIP;
     g_scratch_ptr[dev] = sp;
@@ -537,6 +538,8 @@ int decode_q8(const lorc_layer_desc* desc, Q8Form form, const void* q, const int
                              workspace, workspace_bytes, plan, 0, n_cus))
     return rc;
   p.page_elems = q8_page_bytes(desc->rank_k, desc->rank_v) / 2;
+  p.coded = static_cast<const unsigned char*>(packed) +
+            packed_off_coded_bytes(desc->d_model, desc->rank_k, desc->rank_v, desc->n_kv_heads * desc->head_dim);
   return launch_decode_q8(*desc, form, p, plan, static_cast<hipStream_t>(stream));
 }
 }  // namespace

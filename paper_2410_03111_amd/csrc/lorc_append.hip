@@ -49,6 +49,41 @@ __global__ void pack_factors_kernel(const uint16_t* __restrict__ A_k, const uint
   }
 }
 
+// B_k as pairs of e4m3 codes.  The first is the entry rounded to four significant bits, the second what that leaves: together the eight
+// bits of a bf16 entry, except below 2^-10 of the run's largest code unit, where what is lost is 5e-6 of the run's largest
+// entry at most.  One thread per column and run of 64 latent indices.
+__global__ __launch_bounds__(256) void pack_codes_kernel(const uint16_t* __restrict__ B_k, unsigned char* __restrict__ coded, int r_k, int n) {
+  const int steps = coded_steps(r_k);
+  const int i = blockIdx.x * 256 + threadIdx.x, c = i % n, s = i / n;
+  if (s >= steps) return;
+  float x[64];
+  uint32_t most = 0;
+#pragma unroll
+  for (int k = 0; k < 64; ++k) {
+    const uint32_t b = 64 * s + k < r_k ? B_k[(size_t)(64 * s + k) * n + c] : 0u;
+    x[k] = __uint_as_float(b << 16);
+    const uint32_t a = b & 0x7fffu;
+    if (a < 0x7f80u && a > most) most = a;
+  }
+  int byte = (int)(most >> 7) - 8 + ((most & 0x7f) > 0x60 ? 1 : 0);  // least power of two with |entry| <= 448 of it
+  byte = byte < 1 ? 1 : byte;
+  const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);
+  uint32_t* dst = reinterpret_cast<uint32_t*>(coded) + (size_t)(s * n + c) * 32;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) {  // word w: entries 4 w .. 4 w + 3 of the run
+    const float a0 = x[4 * w] * inv, a1 = x[4 * w + 1] * inv, a2 = x[4 * w + 2] * inv, a3 = x[4 * w + 3] * inv;
+    int hi = __builtin_amdgcn_cvt_pk_fp8_f32(a0, a1, 0, false);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(a2, a3, hi, true);
+    const auto h01 = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), h23 = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
+    int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a0 - h01[0], a1 - h01[1], 0, false);
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(a2 - h23[0], a3 - h23[1], lo, true);
+    const int half = (w >> 1) & 1, at = (w >> 2) * 2 + (w & 1);  // word of the half: 8 i + e, i = w / 4
+    dst[half * 16 + at] = (uint32_t)hi;
+    dst[half * 16 + 8 + at] = (uint32_t)lo;
+  }
+  coded[(size_t)steps * n * 128 + (size_t)c * 8 + s] = (unsigned char)byte;
+}
+
 // ------------------------------------------------------------------------------------------------ append
 // Short prompts.  Block tile: 64 latent rows x 64 tokens, k-tile 64, 4 waves as 2x2; or 32 x 32, each wave a k-step of the k-tile.
 // LDS rows are 64 bf16 = 8 chunks of 16 B; chunk c of row r is stored at c ^ (r & 7) so that the 32 rows a
@@ -754,9 +789,14 @@ int launch_mfma_probe(float* sink, int workgroups, int iters, int operands, hipS
 int launch_pack(const lorc_layer_desc& d, const void* A_k, const void* A_v, const void* B_k, const void* B_v,
                 void* packed, hipStream_t s) {
   const int n = d.n_kv_heads * d.head_dim;
-  return launch_kernel(pack_factors_kernel, dim3(2048), dim3(256), 0, s, (const uint16_t*)A_k, (const uint16_t*)A_v,
-                       (const uint16_t*)B_k, (const uint16_t*)B_v, (uint16_t*)packed, d.d_model, d.rank_k, d.rank_v, n,
-                       d.head_dim, d.rope_base);
+  if (int rc = launch_kernel(pack_factors_kernel, dim3(2048), dim3(256), 0, s, (const uint16_t*)A_k, (const uint16_t*)A_v,
+                             (const uint16_t*)B_k, (const uint16_t*)B_v, (uint16_t*)packed, d.d_model, d.rank_k, d.rank_v, n,
+                             d.head_dim, d.rope_base))
+    return rc;
+  const int steps = coded_steps(d.rank_k);
+  if (steps == 0 || B_k == nullptr) return LORC_OK;
+  return launch_kernel(pack_codes_kernel, dim3((steps * n + 255) / 256), dim3(256), 0, s, (const uint16_t*)B_k,
+                       static_cast<unsigned char*>(packed) + packed_off_coded_bytes(d.d_model, d.rank_k, d.rank_v, n), d.rank_k, n);
 }
 
 int set_kernel_attributes_append() {

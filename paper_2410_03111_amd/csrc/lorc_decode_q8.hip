@@ -445,12 +445,16 @@ DecodePlan make_q8_plan(const lorc_layer_desc& d, Q8Form form, int b, int max_ct
   pl.tile = kPage;
   int n_tiles = (max_ctx + kPage - 1) / kPage;
   if (n_tiles < 1) n_tiles = 1;
-  const long units = form == Q8Form::kAbsorbed ? (d.n_q_heads + 31) / 32 : form == Q8Form::kPlain ? (d.n_kv_heads + 3) / 4 : d.n_kv_heads;
-  long ns = (2L * (n_cus > 0 ? n_cus : 256) + b * units - 1) / (b * units);
+  const bool stationary = form == Q8Form::kRotary && q8_stationary_shape_ok(d);
+  const long units = form == Q8Form::kAbsorbed ? (d.n_q_heads + 31) / 32 : form == Q8Form::kPlain ? (d.n_kv_heads + 3) / 4 :
+                     stationary ? (d.n_kv_heads + 1) / 2 : d.n_kv_heads;
+  pl.stationary = stationary;
+  const long least = stationary ? (n_tiles + q8_stationary_max_tiles() - 1) / q8_stationary_max_tiles() : 1;
+  long ns = ((stationary ? 1L : 2L) * (n_cus > 0 ? n_cus : 256) + b * units - 1) / (b * units);
   if (ns > 64) ns = 64;
   if (ns > max_splits) ns = max_splits;
+  if (ns < least) ns = least;
   if (ns > n_tiles) ns = n_tiles;
-  if (ns < 1) ns = 1;
   pl.tiles_per_split = (int)((n_tiles + ns - 1) / ns);
   pl.n_splits = (n_tiles + pl.tiles_per_split - 1) / pl.tiles_per_split;
   const int out_w = form == Q8Form::kPlain ? d.head_dim : d.rank_v;
@@ -463,10 +467,15 @@ DecodePlan make_q8_plan(const lorc_layer_desc& d, Q8Form form, int b, int max_ct
   return pl;
 }
 
-// A plan of as many splits as a workspace of `bytes` holds (no kernel here needs more than one: a larger call's size always does).
+// A plan of as many splits as a workspace of `bytes` holds.  The fewest that a kernel can do with grow with the context and with b: a
+// larger call's size always holds them.
 DecodePlan make_q8_plan_within(const lorc_layer_desc& d, Q8Form form, int b, int max_ctx, int n_cus, size_t bytes) {
   DecodePlan pl = make_q8_plan(d, form, b, max_ctx, n_cus, kAnySplits);
-  while (pl.total_bytes > bytes && pl.n_splits > 1) pl = make_q8_plan(d, form, b, max_ctx, n_cus, pl.n_splits - 1);
+  while (pl.total_bytes > bytes && pl.n_splits > 1) {
+    const DecodePlan fewer = make_q8_plan(d, form, b, max_ctx, n_cus, pl.n_splits - 1);
+    if (fewer.n_splits >= pl.n_splits) break;  // the fewest that the kernel can walk
+    pl = fewer;
+  }
   return pl;
 }
 
@@ -484,6 +493,10 @@ int launch_decode_q8(const lorc_layer_desc& d, Q8Form form, const DecodeParams& 
     const dim3 grid(units * ((n_units + 3) / 4));
     if (int rc = launch_kernel(p.G > 16 ? decode_plain_q8_kernel<true> : decode_plain_q8_kernel<false>, grid, dim3(256), 0, s, p)) return rc;
     return launch_decode_merge(p, true, s);
+  }
+  if (plan.stationary) {
+    if (int rc = launch_decode_q8_stationary(p, s)) return rc;
+    return launch_decode_merge(p, false, s);
   }
   const size_t lds = q8_lds_bytes(d);
   if (lds > 160 * 1024) return LORC_EUNSUPPORTED;

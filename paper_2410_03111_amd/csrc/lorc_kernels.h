@@ -64,6 +64,7 @@ struct DecodeParams {
   const int32_t* ctx_len;   // [b]
   const uint16_t* bk;       // packed B_k tiles
   const uint16_t* bv;       // packed B_v tiles
+  const unsigned char* coded;  // packed: B_k as pairs of e4m3 codes (decode over 8-bit pages)
   const uint16_t* cache;
   const int32_t* block_table;
   uint16_t* out;            // [b x h_q x d], or [b x h_q x r_v] when latent_out is set
@@ -184,6 +185,11 @@ DecodePlan make_q8_plan(const lorc_layer_desc& d, Q8Form form, int b, int max_ct
 DecodePlan make_q8_plan_within(const lorc_layer_desc& d, Q8Form form, int b, int max_ctx, int n_cus, size_t bytes);
 int launch_decode_q8(const lorc_layer_desc& d, Q8Form form, const DecodeParams& p, const DecodePlan& plan, hipStream_t s);
 int set_kernel_attributes_decode_q8();
+// Rotary form with the key factor in registers (lorc_decode_q8_stat.hip).
+bool q8_stationary_shape_ok(const lorc_layer_desc& d);
+int q8_stationary_max_tiles();  // pages that a split of it walks at most
+int set_kernel_attributes_decode_q8_stationary();
+int launch_decode_q8_stationary(const DecodeParams& p, hipStream_t s);
 // The merge that follows a split kernel; plain: partial rows of head_dim coordinates that no factor is applied to.
 int launch_decode_merge(const DecodeParams& p, bool plain, hipStream_t s);
 

@@ -85,8 +85,18 @@ constexpr size_t kRopeTabBytes = 64 * 8 + 32 * 64 * 8;
 LORC_HD size_t packed_off_rope(int D, int r_k, int r_v, int n) {
   return packed_off_at_tiled(D, r_k, r_v, n) + packed_at_elems(D, r_k, r_v);
 }
+// B_k once more for the decode over 8-bit pages (key ranks up to 512): every bf16 entry as the sum of two e4m3 codes under one power of
+// two per column and 64 latent indices.  Codes [j/64][column][half][first, second][32]: byte 8 i + e of a half is latent index
+// 64 (j/64) + 16 i + 8 half + e; then the scale bytes (exponent + 127) [column][8] of the up to eight runs of 64.
+constexpr int kCodedMaxRank = 512;
+LORC_HD int coded_steps(int r_k) { return r_k <= kCodedMaxRank ? (r_k + 63) / 64 : 0; }
+LORC_HD size_t packed_off_coded_bytes(int D, int r_k, int r_v, int n) {
+  return ((packed_off_rope(D, r_k, r_v, n) * 2 + kRopeTabBytes) + 255) & ~(size_t)255;
+}
 LORC_HD size_t packed_total_elems(int D, int r_k, int r_v, int n) {
-  return packed_off_rope(D, r_k, r_v, n) + kRopeTabBytes / 2;
+  const size_t steps = coded_steps(r_k);
+  if (steps == 0) return packed_off_rope(D, r_k, r_v, n) + kRopeTabBytes / 2;
+  return (packed_off_coded_bytes(D, r_k, r_v, n) + steps * n * 128 + (size_t)n * 8) / 2;
 }
 
 }  // namespace lorc
