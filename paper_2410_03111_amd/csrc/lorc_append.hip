@@ -4,6 +4,7 @@
 // operands, fp32 accumulation on the 32x32x16 matrix-core op, RNE to bf16, scattered into the tiled pages.
 #include "lorc_device.h"
 #include "lorc_kernels.h"
+#include "lorc_q8.h"
 #include "lorc_rebuild.h"
 #include "lorc_tile_product.h"
 
@@ -62,21 +63,16 @@ __global__ __launch_bounds__(256) void pack_codes_kernel(const uint16_t* __restr
   for (int k = 0; k < 64; ++k) {
     const uint32_t b = 64 * s + k < r_k ? B_k[(size_t)(64 * s + k) * n + c] : 0u;
     x[k] = __uint_as_float(b << 16);
-    const uint32_t a = b & 0x7fffu;
-    if (a < 0x7f80u && a > most) most = a;
+    const uint32_t a = magnitude(b);
+    most = most > a ? most : a;
   }
-  int byte = (int)(most >> 7) - 8 + ((most & 0x7f) > 0x60 ? 1 : 0);  // least power of two with |entry| <= 448 of it
-  byte = byte < 1 ? 1 : byte;
-  const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);
+  const int byte = scale_byte(most);
+  const float inv = inverse_scale(byte);
   uint32_t* dst = reinterpret_cast<uint32_t*>(coded) + (size_t)(s * n + c) * 32;
 #pragma unroll
   for (int w = 0; w < 16; ++w) {  // word w: entries 4 w .. 4 w + 3 of the run
-    const float a0 = x[4 * w] * inv, a1 = x[4 * w + 1] * inv, a2 = x[4 * w + 2] * inv, a3 = x[4 * w + 3] * inv;
-    int hi = __builtin_amdgcn_cvt_pk_fp8_f32(a0, a1, 0, false);
-    hi = __builtin_amdgcn_cvt_pk_fp8_f32(a2, a3, hi, true);
-    const auto h01 = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), h23 = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
-    int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a0 - h01[0], a1 - h01[1], 0, false);
-    lo = __builtin_amdgcn_cvt_pk_fp8_f32(a2 - h23[0], a3 - h23[1], lo, true);
+    int hi, lo;
+    code_pair(x[4 * w] * inv, x[4 * w + 1] * inv, x[4 * w + 2] * inv, x[4 * w + 3] * inv, hi, lo);
     const int half = (w >> 1) & 1, at = (w >> 2) * 2 + (w & 1);  // word of the half: 8 i + e, i = w / 4
     dst[half * 16 + at] = (uint32_t)hi;
     dst[half * 16 + 8 + at] = (uint32_t)lo;

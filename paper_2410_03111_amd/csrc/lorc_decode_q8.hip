@@ -9,45 +9,13 @@
 // bounds l; values below 448 x 2^kLeastExp are far below what the fp16 partials hold.)
 #include "lorc_device.h"
 #include "lorc_kernels.h"
+#include "lorc_q8.h"
 
 namespace lorc {
 
 namespace {
 constexpr float kNegInfQ = -__builtin_huge_valf();
-constexpr int kLeastExp = -40;
 constexpr double kTurns = 0.15915494309189533576888;  // 1 / 2 pi
-typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-
-__device__ __forceinline__ float pow2_of(uint32_t byte) { return __uint_as_float(byte << 23); }  // 2^(byte - 127)
-
-// eight codes (two words) times a power of two, as fp16 or as bf16
-__device__ __forceinline__ f16x8 codes_f16(u32x2 v, float scale = 1.f) {
-  u32x4 r;
-  const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)v[0], scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)v[0], scale, true);
-  const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)v[1], scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)v[1], scale, true);
-  r[0] = __builtin_bit_cast(uint32_t, a);
-  r[1] = __builtin_bit_cast(uint32_t, b);
-  r[2] = __builtin_bit_cast(uint32_t, c);
-  r[3] = __builtin_bit_cast(uint32_t, d);
-  return __builtin_bit_cast(f16x8, r);
-}
-__device__ __forceinline__ u32x4 codes_bf16(u32x2 v, float scale) {
-  u32x4 r;
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)v[0], scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)v[0], scale, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)v[1], scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)v[1], scale, true);
-  r[0] = __builtin_bit_cast(uint32_t, a);
-  r[1] = __builtin_bit_cast(uint32_t, b);
-  r[2] = __builtin_bit_cast(uint32_t, c);
-  r[3] = __builtin_bit_cast(uint32_t, d);
-  return r;
-}
-// the first n of eight bytes
-__device__ __forceinline__ u32x2 keep_bytes(u32x2 v, int n) {
-  n = n < 0 ? 0 : (n > 8 ? 8 : n);
-  const uint64_t m = n == 8 ? ~0ull : (1ull << (8 * n)) - 1ull;
-  return u32x2{v[0] & (uint32_t)m, v[1] & (uint32_t)(m >> 32)};
-}
 }  // namespace
 
 // ------------------------------------------------------------------------------------------------ any shape
@@ -112,7 +80,7 @@ __global__ __launch_bounds__(256, 1) void decode_q8_kernel(DecodeParams p) {
       for (int h = tid / HALF; h < nh; h += 256 / HALF) {
         const uint16_t* src = p.q + ((size_t)seq * p.h_q + h0 + h) * HD + i;
         const float x = bf16_to_float(src[0]) * p.q_scale, y = bf16_to_float(src[HALF]) * p.q_scale;
-        f16x2 v;
+        half2_t v;
         v[0] = static_cast<_Float16>(x * cs - y * sn);
         v[1] = static_cast<_Float16>(y * cs + x * sn);
         qr[h * HALF + i] = __builtin_bit_cast(uint32_t, v);
@@ -445,12 +413,13 @@ DecodePlan make_q8_plan(const lorc_layer_desc& d, Q8Form form, int b, int max_ct
   pl.tile = kPage;
   int n_tiles = (max_ctx + kPage - 1) / kPage;
   if (n_tiles < 1) n_tiles = 1;
-  const bool stationary = form == Q8Form::kRotary && q8_stationary_shape_ok(d);
+  const bool stationary = form == Q8Form::kRotary && q8_stationary_shape_ok(d), absorbed = form == Q8Form::kAbsorbed && q8_absorbed_shape_ok(d);
   const long units = form == Q8Form::kAbsorbed ? (d.n_q_heads + 31) / 32 : form == Q8Form::kPlain ? (d.n_kv_heads + 3) / 4 :
                      stationary ? (d.n_kv_heads + 1) / 2 : d.n_kv_heads;
-  pl.stationary = stationary;
-  const long least = stationary ? (n_tiles + q8_stationary_max_tiles() - 1) / q8_stationary_max_tiles() : 1;
-  long ns = ((stationary ? 1L : 2L) * (n_cus > 0 ? n_cus : 256) + b * units - 1) / (b * units);
+  pl.stationary = stationary || absorbed;
+  const int most = stationary ? q8_stationary_max_tiles() : absorbed ? q8_absorbed_max_tiles() : n_tiles;
+  const long least = (n_tiles + most - 1) / most;
+  long ns = ((stationary || absorbed ? 1L : 2L) * (n_cus > 0 ? n_cus : 256) + b * units - 1) / (b * units);
   if (ns > 64) ns = 64;
   if (ns > max_splits) ns = max_splits;
   if (ns < least) ns = least;
@@ -495,7 +464,7 @@ int launch_decode_q8(const lorc_layer_desc& d, Q8Form form, const DecodeParams& 
     return launch_decode_merge(p, true, s);
   }
   if (plan.stationary) {
-    if (int rc = launch_decode_q8_stationary(p, s)) return rc;
+    if (int rc = form == Q8Form::kAbsorbed ? launch_decode_q8_absorbed(p, s) : launch_decode_q8_stationary(p, s)) return rc;
     return launch_decode_merge(p, false, s);
   }
   const size_t lds = q8_lds_bytes(d);

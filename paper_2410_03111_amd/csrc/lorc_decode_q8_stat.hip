@@ -16,14 +16,13 @@
 // values' scales: see lorc_decode_q8.hip.
 #include "lorc_device.h"
 #include "lorc_kernels.h"
+#include "lorc_q8.h"
 #include "lorc_stationary.h"
 
 namespace lorc {
 
 namespace {
-typedef __attribute__((ext_vector_type(8))) int i32x8;
 constexpr int kQ8Tiles = 128;      // pages a workgroup walks at most (their ids live in LDS)
-constexpr int kQ8LeastExp = -40;   // see lorc_decode_q8.hip
 constexpr int kQ8ScaleBytes = 256; // scale bytes of a tile's K (or V) codes: up to four groups
 
 __host__ __device__ inline size_t q8_stat_lds_bytes(int ns, int r_v, int heads) {
@@ -39,24 +38,6 @@ __host__ __device__ inline size_t q8_stat_lds_bytes(int ns, int r_v, int heads) 
   return b;
 }
 
-// A copy of 256 bytes global -> LDS, four per lane (see dma_1k).
-__device__ __forceinline__ void dma_256(u32x4 rsrc, uint32_t lds_off, uint32_t lane4, uint32_t soff) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds"
-               :
-               : "s"(lds_off), "v"(lane4), "s"(rsrc), "s"(soff)
-               : "memory");
-}
-
-__device__ __forceinline__ f16x8 q8_f16(uint32_t a, uint32_t b) {
-  u32x4 r;
-  const f16x2 v0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)a, 1.f, false), v1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)a, 1.f, true);
-  const f16x2 v2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)b, 1.f, false), v3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)b, 1.f, true);
-  r[0] = __builtin_bit_cast(uint32_t, v0);
-  r[1] = __builtin_bit_cast(uint32_t, v1);
-  r[2] = __builtin_bit_cast(uint32_t, v2);
-  r[3] = __builtin_bit_cast(uint32_t, v3);
-  return __builtin_bit_cast(f16x8, r);
-}
 __device__ __forceinline__ f32x4s mfma16_f16(f16x8 a, f16x8 b, f32x4s c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 }  // namespace
 
@@ -119,7 +100,6 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
 
-  auto uniform = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane(v); };
   // ---- copies of a tile: blocks of 1 KiB, wave w moves w, w + 8, ...
   const uint32_t lane16 = (uint32_t)lane * 16u;
   const int k_rows = r_k >> 5, k_blocks = 2 * k_rows, v_blocks = r_v >> 4;
@@ -137,18 +117,18 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
 #pragma unroll
     for (int i = 0; i < (4 * NS + NW - 1) / NW; ++i) {
       const int b = w + NW * i, pb = b >= k_rows ? 1 : 0, c = b - pb * k_rows;
-      if (b < k_blocks) dma_1k(r, uniform(k_lds + (uint32_t)(buf * NS * 4096 + pb * NS * 2048 + c * 1024)), lane16, uniform((uint32_t)b * 1024u));
+      if (b < k_blocks) dma_1k(r, uniform_u32(k_lds + (uint32_t)(buf * NS * 4096 + pb * NS * 2048 + c * 1024)), lane16, uniform_u32((uint32_t)b * 1024u));
     }
-    if (w == 0) dma_256(r, uniform(s_lds + (uint32_t)(buf * kQ8ScaleBytes)), lane16 >> 2, uniform((uint32_t)(64 * (r_k + r_v))));
+    if (w == 0) dma_256(r, uniform_u32(s_lds + (uint32_t)(buf * kQ8ScaleBytes)), lane16 >> 2, uniform_u32((uint32_t)(64 * (r_k + r_v))));
   };
   auto copy_v = [&](int id, int buf) {
     const u32x4 r = rsrc_of(id);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int b = w + NW * i;
-      if (b < v_blocks) dma_1k(r, uniform(v_lds + (uint32_t)(buf * 64 * r_v + b * 1024)), lane16, uniform((uint32_t)(64 * r_k + b * 1024)));
+      if (b < v_blocks) dma_1k(r, uniform_u32(v_lds + (uint32_t)(buf * 64 * r_v + b * 1024)), lane16, uniform_u32((uint32_t)(64 * r_k + b * 1024)));
     }
-    if (w == NW - 1) dma_256(r, uniform(s_lds + (uint32_t)((2 + buf) * kQ8ScaleBytes)), lane16 >> 2, uniform((uint32_t)(64 * (r_k + r_v + gk))));
+    if (w == NW - 1) dma_256(r, uniform_u32(s_lds + (uint32_t)((2 + buf) * kQ8ScaleBytes)), lane16 >> 2, uniform_u32((uint32_t)(64 * (r_k + r_v + gk))));
   };
 
   // ---- what stays in registers
@@ -264,7 +244,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
     uint32_t top = sm.ub[0] > sm.ub[1] ? sm.ub[0] : sm.ub[1];
     const uint32_t t2 = sm.ub[2] > sm.ub[3] ? sm.ub[2] : sm.ub[3];
     top = top > t2 ? top : t2;
-    top = top > 127 + kQ8LeastExp ? top : 127 + kQ8LeastExp;
+    top = top > 127 + kLeastExp ? top : 127 + kLeastExp;
     sm.mx = sm.s + ((float)top - 127.f);
   };
   auto softmax_rows = [&](Softmax& sm) {
@@ -322,8 +302,8 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
         v[3] &= (uint32_t)(keep >> 32);
       }
       const f16x8 pf = load_frag_f16(p_src + ph * 512);
-      o[2 * jb] = mfma16_f16(pf, q8_f16(v[0], v[1]), o[2 * jb]);
-      o[2 * jb + 1] = mfma16_f16(pf, q8_f16(v[2], v[3]), o[2 * jb + 1]);
+      o[2 * jb] = mfma16_f16(pf, codes_f16(u32x2{v[0], v[1]}), o[2 * jb]);
+      o[2 * jb + 1] = mfma16_f16(pf, codes_f16(u32x2{v[2], v[3]}), o[2 * jb + 1]);
     }
   };
   using I0 = std::integral_constant<int, 0>;

@@ -190,6 +190,11 @@ bool q8_stationary_shape_ok(const lorc_layer_desc& d);
 int q8_stationary_max_tiles();  // pages that a split of it walks at most
 int set_kernel_attributes_decode_q8_stationary();
 int launch_decode_q8_stationary(const DecodeParams& p, hipStream_t s);
+// Absorbed form up to rank 512 (lorc_decode_q8_abs.hip).
+bool q8_absorbed_shape_ok(const lorc_layer_desc& d);
+int q8_absorbed_max_tiles();
+int set_kernel_attributes_decode_q8_absorbed();
+int launch_decode_q8_absorbed(const DecodeParams& p, hipStream_t s);
 // The merge that follows a split kernel; plain: partial rows of head_dim coordinates that no factor is applied to.
 int launch_decode_merge(const DecodeParams& p, bool plain, hipStream_t s);
 

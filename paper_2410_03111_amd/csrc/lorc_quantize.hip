@@ -12,21 +12,11 @@
 // Bound by memory: 2 bytes read and 1 written per latent (+ 1 per 128).
 #include "lorc_device.h"
 #include "lorc_kernels.h"
+#include "lorc_q8.h"
 
 namespace lorc {
 
 namespace {
-// exponent byte of a group whose largest finite magnitude has the bf16 bits `a` (no sign): 1.75 x 2^8 is the largest code
-__device__ __forceinline__ int scale_byte(uint32_t a) {
-  const int e = (int)(a >> 7) - 8 + ((a & 0x7f) > 0x60 ? 1 : 0);
-  return e < 1 ? 1 : e;
-}
-__device__ __forceinline__ float inverse_scale(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
-// magnitude bits of the two bf16 of a word, 0 where they are inf or NaN
-__device__ __forceinline__ uint32_t magnitude(uint32_t half) {
-  const uint32_t a = half & 0x7fffu;
-  return a < 0x7f80u ? a : 0u;
-}
 __device__ __forceinline__ uint32_t max_half(uint32_t v) {  // over the two halves of the wave
   const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
   const uint32_t a = r[0], b = r[1];
