@@ -467,70 +467,109 @@ def pages_workspace_bytes(n_seqs: int, n_pages: int) -> int:
     return _lib.lorc_pages_workspace_bytes(n_seqs, n_pages)
 
 
-def _table(block_table, page_refs):
-    _dev(block_table, torch.int32, "block_table")
-    _dev(page_refs, torch.int32, "page_refs")
-    n_seqs, max_pages = block_table.shape
-    return (_ptr(block_table), n_seqs, max_pages, _ptr(page_refs), page_refs.numel())
+# The calls below launch one or two kernels of a few microseconds, so that their checks are one pass over the tensors (a pair of calls
+# with twelve tensors: 23 -> 19 us of host time).
+def _refuse(t, dtype, name, dev):
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != dev:
+        raise ValueError(f"{name}: on device {t.get_device()}, the current one is {dev}")
+    raise TypeError(f"{name}: expected a contiguous CUDA tensor of dtype {dtype}")
 
 
-def _lists(n, **lists):
-    for name, t in lists.items():
-        _dev(t, torch.int32, name)
-        assert t.numel() == n, name
+def _on_device(dtype, dev, names, *tensors):
+    """Every tensor contiguous, of this dtype and on the current device."""
+    for i, t in enumerate(tensors):
+        try:
+            ok = t.get_device() == dev and t.dtype is dtype and t.is_contiguous()
+        except AttributeError:
+            ok = False
+        if not ok:
+            _refuse(t, dtype, names[i], dev)
 
 
-def _pages_workspace(block_table, page_refs, workspace):
+def _same_length(n, names, *tensors):
+    for i, t in enumerate(tensors):
+        if t.numel() != n:
+            raise ValueError(f"{names[i]}: {t.numel()} entries, expected {n}")
+
+
+def _pages_workspace(block_table, page_refs, workspace, dev):
     if workspace is None:
-        workspace = torch.empty(pages_workspace_bytes(block_table.shape[0], page_refs.numel()), dtype=torch.uint8, device=block_table.device)
-    return _dev(workspace, torch.uint8, "workspace")
+        return torch.empty(pages_workspace_bytes(block_table.shape[0], page_refs.numel()), dtype=torch.uint8, device=block_table.device)
+    _on_device(torch.uint8, dev, ("workspace",), workspace)
+    return workspace
 
 
 def copy_pages(pool, src, dst, page_bytes=None):
     """Pool page src[i] -> dst[i] (see lorc_copy_pages).  pool: any contiguous tensor whose first dimension is the page, or a flat one
     with the bytes of a page; src, dst int32, pairs with an id outside the pool are skipped."""
-    if not (isinstance(pool, torch.Tensor) and pool.is_cuda and pool.is_contiguous()):
-        raise TypeError("pool: expected a contiguous CUDA tensor")
+    dev = torch._C._cuda_getDevice()
+    _on_device(pool.dtype if isinstance(pool, torch.Tensor) else None, dev, ("pool",), pool)
+    _on_device(torch.int32, dev, ("src", "dst"), src, dst)
+    n = src.numel()
+    _same_length(n, ("dst",), dst)
     total = pool.numel() * pool.element_size()
     if page_bytes is None:
         page_bytes = total // pool.shape[0]
-    _lists(src.numel(), src=src, dst=dst)
-    _check(_lib.lorc_copy_pages(_ptr(pool), page_bytes, total // page_bytes if page_bytes > 0 else 0, _ptr(src), _ptr(dst), src.numel(),
-                                _stream()), "lorc_copy_pages")
+    _check(_lib.lorc_copy_pages(pool.data_ptr(), page_bytes, total // page_bytes if page_bytes > 0 else 0, src.data_ptr(), dst.data_ptr(), n,
+                                torch._C._cuda_getCurrentRawStream(dev)), "lorc_copy_pages")
+
+
+_FORK = ("block_table", "page_refs", "parents", "children", "lens", "copy_src", "copy_dst", "status")
 
 
 def fork_sequences(block_table, page_refs, parents, children, lens, copy_src, copy_dst, status, workspace=None):
     """Rows children[i] continue the first lens[i] positions of rows parents[i] (see lorc_fork_sequences); copy_src, copy_dst, status [n]
     int32 are written: the pages to copy (copy_pages takes them) and what became of each pair."""
+    dev = torch._C._cuda_getDevice()
+    _on_device(torch.int32, dev, _FORK, block_table, page_refs, parents, children, lens, copy_src, copy_dst, status)
     n = parents.numel()
-    _lists(n, parents=parents, children=children, lens=lens, copy_src=copy_src, copy_dst=copy_dst, status=status)
-    workspace = _pages_workspace(block_table, page_refs, workspace)
-    _check(_lib.lorc_fork_sequences(*_table(block_table, page_refs), _ptr(parents), _ptr(children), _ptr(lens), n, _ptr(copy_src),
-                                    _ptr(copy_dst), _ptr(status), _ptr(workspace), workspace.numel(), _stream()), "lorc_fork_sequences")
+    _same_length(n, _FORK[3:], children, lens, copy_src, copy_dst, status)
+    workspace = _pages_workspace(block_table, page_refs, workspace, dev)
+    n_seqs, max_pages = block_table.shape
+    _check(_lib.lorc_fork_sequences(block_table.data_ptr(), n_seqs, max_pages, page_refs.data_ptr(), page_refs.numel(), parents.data_ptr(),
+                                    children.data_ptr(), lens.data_ptr(), n, copy_src.data_ptr(), copy_dst.data_ptr(), status.data_ptr(),
+                                    workspace.data_ptr(), workspace.numel(), torch._C._cuda_getCurrentRawStream(dev)), "lorc_fork_sequences")
 
 
 def free_sequences(block_table, page_refs, seqs):
     """Releases the rows (see lorc_free_sequences)."""
-    _dev(seqs, torch.int32, "seqs")
-    _check(_lib.lorc_free_sequences(*_table(block_table, page_refs), _ptr(seqs), seqs.numel(), _stream()), "lorc_free_sequences")
+    dev = torch._C._cuda_getDevice()
+    _on_device(torch.int32, dev, ("block_table", "page_refs", "seqs"), block_table, page_refs, seqs)
+    n_seqs, max_pages = block_table.shape
+    _check(_lib.lorc_free_sequences(block_table.data_ptr(), n_seqs, max_pages, page_refs.data_ptr(), page_refs.numel(), seqs.data_ptr(),
+                                    seqs.numel(), torch._C._cuda_getCurrentRawStream(dev)), "lorc_free_sequences")
+
+
+_COMPACT = ("block_table", "page_refs", "move_src", "move_dst", "page_map")
 
 
 def compact_pages(block_table, page_refs, move_src, move_dst, page_map):
     """Makes the pool dense with at most move_src.numel() moves (see lorc_compact_pages); move_src, move_dst and page_map [n_pages] int32 are
     written, the pages' contents are the caller's to move (copy_pages)."""
-    _lists(move_src.numel(), move_src=move_src, move_dst=move_dst)
-    _lists(page_refs.numel(), page_map=page_map)
-    _check(_lib.lorc_compact_pages(*_table(block_table, page_refs), _ptr(move_src), _ptr(move_dst), move_src.numel(), _ptr(page_map),
-                                   _stream()), "lorc_compact_pages")
+    dev = torch._C._cuda_getDevice()
+    _on_device(torch.int32, dev, _COMPACT, block_table, page_refs, move_src, move_dst, page_map)
+    n_pages, moves = page_refs.numel(), move_src.numel()
+    _same_length(moves, ("move_dst",), move_dst)
+    _same_length(n_pages, ("page_map",), page_map)
+    n_seqs, max_pages = block_table.shape
+    _check(_lib.lorc_compact_pages(block_table.data_ptr(), n_seqs, max_pages, page_refs.data_ptr(), n_pages, move_src.data_ptr(),
+                                   move_dst.data_ptr(), moves, page_map.data_ptr(), torch._C._cuda_getCurrentRawStream(dev)), "lorc_compact_pages")
+
+
+_RESERVE = ("block_table", "page_refs", "seqs", "lens", "status")
 
 
 def reserve_pages(block_table, page_refs, seqs, lens, status, workspace=None):
     """Gives rows seqs[i] pages for their first lens[i] positions (see lorc_reserve_pages); status [n] int32 is written."""
+    dev = torch._C._cuda_getDevice()
+    _on_device(torch.int32, dev, _RESERVE, block_table, page_refs, seqs, lens, status)
     n = seqs.numel()
-    _lists(n, seqs=seqs, lens=lens, status=status)
-    workspace = _pages_workspace(block_table, page_refs, workspace)
-    _check(_lib.lorc_reserve_pages(*_table(block_table, page_refs), _ptr(seqs), _ptr(lens), n, _ptr(status), _ptr(workspace),
-                                   workspace.numel(), _stream()), "lorc_reserve_pages")
+    _same_length(n, _RESERVE[3:], lens, status)
+    workspace = _pages_workspace(block_table, page_refs, workspace, dev)
+    n_seqs, max_pages = block_table.shape
+    _check(_lib.lorc_reserve_pages(block_table.data_ptr(), n_seqs, max_pages, page_refs.data_ptr(), page_refs.numel(), seqs.data_ptr(),
+                                   lens.data_ptr(), n, status.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                   torch._C._cuda_getCurrentRawStream(dev)), "lorc_reserve_pages")
 
 
 # ---- 8-bit cache
@@ -546,22 +585,27 @@ def cache_scale_index_v(desc: LayerDesc, slot: int, j: int) -> int:
     return _lib.lorc_cache_scale_index_v(ctypes.byref(desc), slot, j)
 
 
+_QUANTIZE = ("block_table", "pos_begin", "pos_end", "block_table_q8")
+
+
 def quantize_latents(desc: LayerDesc, cache, block_table, pos_begin, pos_end, max_tokens, cache_q8, block_table_q8):
     """Positions [pos_begin[s], pos_end[s]) of every sequence from the bf16 pool into the 8-bit pool (see lorc_quantize_latents); max_tokens:
     host bound of their number per sequence."""
-    _dev(cache, torch.uint8, "cache")
-    _dev(cache_q8, torch.uint8, "cache_q8")
-    _dev(block_table, torch.int32, "block_table")
-    _dev(block_table_q8, torch.int32, "block_table_q8")
+    dev = torch._C._cuda_getDevice()
+    _on_device(torch.uint8, dev, ("cache", "cache_q8"), cache, cache_q8)
+    _on_device(torch.int32, dev, _QUANTIZE, block_table, pos_begin, pos_end, block_table_q8)
     b = pos_begin.numel()
-    _lists(b, pos_begin=pos_begin, pos_end=pos_end)
-    assert block_table.shape[0] >= b and block_table_q8.shape[0] >= b
-    page, page_q8 = page_bytes(desc), page_bytes_quantized(desc)
+    _same_length(b, ("pos_end",), pos_end)
+    (rows, max_pages), (rows_q8, max_pages_q8) = block_table.shape, block_table_q8.shape
+    if rows < b or rows_q8 < b:
+        raise ValueError(f"block_table, block_table_q8: {rows} and {rows_q8} rows for {b} sequences")
+    page = page_bytes(desc)
     if page == 0:
         raise LorcError(EUNSUPPORTED, "lorc_page_bytes")
-    _check(_lib.lorc_quantize_latents(ctypes.byref(desc), _ptr(cache), _ptr(block_table), block_table.shape[1], cache.numel() // page,
-                                      _ptr(pos_begin), _ptr(pos_end), b, max_tokens, _ptr(cache_q8), _ptr(block_table_q8),
-                                      block_table_q8.shape[1], cache_q8.numel() // page_q8, _stream()), "lorc_quantize_latents")
+    _check(_lib.lorc_quantize_latents(ctypes.byref(desc), cache.data_ptr(), block_table.data_ptr(), max_pages, cache.numel() // page,
+                                      pos_begin.data_ptr(), pos_end.data_ptr(), b, max_tokens, cache_q8.data_ptr(), block_table_q8.data_ptr(),
+                                      max_pages_q8, cache_q8.numel() // page_bytes_quantized(desc), torch._C._cuda_getCurrentRawStream(dev)),
+           "lorc_quantize_latents")
 
 
 def decode_quantized_workspace_bytes(desc: LayerDesc, b: int, max_ctx: int) -> int:
@@ -576,46 +620,58 @@ def decode_absorbed_quantized_workspace_bytes(desc: LayerDesc, b: int, max_ctx: 
     return _lib.lorc_decode_absorbed_quantized_workspace_bytes(ctypes.byref(desc), b, max_ctx)
 
 
-def _decode_quantized(name, size, desc, q, width, positions, ctx_len, max_ctx, packed, cache, block_table, out, workspace):
-    _dev(q, torch.bfloat16, "q")
-    for t, nm in ((ctx_len, "ctx_len"), (block_table, "block_table"), *positions):
-        _dev(t, torch.int32, nm)
-    _dev(cache, torch.uint8, "cache")
-    b = q.shape[0]
-    assert tuple(q.shape) == (b, desc.n_q_heads, width) and ctx_len.numel() == b and all(t.numel() == b for t, _ in positions)
-    n_seqs, max_pages = block_table.shape
-    assert n_seqs >= b
+def _decode_quantized(name, call, size, desc, q, width, q_pos, ctx_len, max_ctx, packed, cache, block_table, out, workspace):
+    dev = torch._C._cuda_getDevice()
+    _on_device(torch.bfloat16, dev, ("q",), q)
+    _on_device(torch.int32, dev, ("ctx_len", "block_table"), ctx_len, block_table)
+    _on_device(torch.uint8, dev, ("cache_q8", "packed"), cache, packed)
+    b, rows_max = q.shape[0], block_table.shape
+    if tuple(q.shape) != (b, desc.n_q_heads, width) or rows_max[0] < b:
+        raise ValueError(f"q {tuple(q.shape)}, block_table {tuple(rows_max)}: expected [b, {desc.n_q_heads}, {width}] and [>= b, pages]")
+    _same_length(b, ("ctx_len",), ctx_len)
+    if q_pos is not None:
+        _on_device(torch.int32, dev, ("q_pos",), q_pos)
+        _same_length(b, ("q_pos",), q_pos)
     if workspace is None:
         workspace = torch.empty(max(size(ctypes.byref(desc), b, max_ctx), 256), dtype=torch.uint8, device=q.device)
+    else:
+        _on_device(torch.uint8, dev, ("workspace",), workspace)
     if out is None:
         out = torch.empty(b, desc.n_q_heads, desc.head_dim, dtype=torch.bfloat16, device=q.device)
+    else:
+        _on_device(torch.bfloat16, dev, ("out",), out)
+        _same_length(b * desc.n_q_heads * desc.head_dim, ("out",), out)
     page = page_bytes_quantized(desc)
     if page == 0:
         raise LorcError(EUNSUPPORTED, "lorc_page_bytes_quantized")
-    _check(getattr(_lib, name)(ctypes.byref(desc), _ptr(q), *(_ptr(t) for t, _ in positions), _ptr(ctx_len), b, max_ctx, _ptr(packed),
-                               _ptr(cache), _ptr(block_table), max_pages, cache.numel() // page, _ptr(out), _ptr(workspace),
-                               workspace.numel(), _stream()), name)
+    query = (q.data_ptr(),) if q_pos is None else (q.data_ptr(), q_pos.data_ptr())
+    _check(call(ctypes.byref(desc), *query, ctx_len.data_ptr(), b, max_ctx, packed.data_ptr(), cache.data_ptr(), block_table.data_ptr(),
+                rows_max[1], cache.numel() // page, out.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                torch._C._cuda_getCurrentRawStream(dev)), name)
     return out
 
 
 def decode_attention_quantized(desc: LayerDesc, q, q_pos, ctx_len, max_ctx, packed, cache_q8, block_table, out=None, workspace=None):
     """decode_attention over an 8-bit pool."""
-    return _decode_quantized("lorc_decode_attention_quantized", _lib.lorc_decode_quantized_workspace_bytes, desc, q, desc.head_dim,
-                             ((q_pos, "q_pos"),), ctx_len, max_ctx, packed, cache_q8, block_table, out, workspace)
+    return _decode_quantized("lorc_decode_attention_quantized", _lib.lorc_decode_attention_quantized,
+                             _lib.lorc_decode_quantized_workspace_bytes, desc, q, desc.head_dim, q_pos, ctx_len, max_ctx, packed, cache_q8,
+                             block_table, out, workspace)
 
 
 def decode_attention_plain_quantized(desc: LayerDesc, q, q_pos, ctx_len, max_ctx, packed, cache_q8, block_table, out=None,
                                      workspace=None):
     """decode_attention_plain (an uncompressed layer) over an 8-bit pool."""
-    return _decode_quantized("lorc_decode_attention_plain_quantized", _lib.lorc_decode_plain_quantized_workspace_bytes, desc, q,
-                             desc.head_dim, ((q_pos, "q_pos"),), ctx_len, max_ctx, packed, cache_q8, block_table, out, workspace)
+    return _decode_quantized("lorc_decode_attention_plain_quantized", _lib.lorc_decode_attention_plain_quantized,
+                             _lib.lorc_decode_plain_quantized_workspace_bytes, desc, q, desc.head_dim, q_pos, ctx_len, max_ctx, packed,
+                             cache_q8, block_table, out, workspace)
 
 
 def decode_attention_absorbed_quantized(desc: LayerDesc, q_lat, ctx_len, max_ctx, packed, cache_q8, block_table, out=None,
                                         workspace=None):
     """decode_attention_absorbed (no rotation, key factor folded into the query) over an 8-bit pool."""
-    return _decode_quantized("lorc_decode_attention_absorbed_quantized", _lib.lorc_decode_absorbed_quantized_workspace_bytes, desc, q_lat,
-                             desc.rank_k, (), ctx_len, max_ctx, packed, cache_q8, block_table, out, workspace)
+    return _decode_quantized("lorc_decode_attention_absorbed_quantized", _lib.lorc_decode_attention_absorbed_quantized,
+                             _lib.lorc_decode_absorbed_quantized_workspace_bytes, desc, q_lat, desc.rank_k, None, ctx_len, max_ctx, packed,
+                             cache_q8, block_table, out, workspace)
 
 
 def mfma_rate_probe(sink, workgroups: int, iters: int, operands: int = 0):

@@ -6,7 +6,8 @@
 // What bounds these calls is the chain of launches and of trips to memory, not the bytes: so each is a plan (one workgroup of
 // 1024 threads that walks the counts 16 to a thread and ranks by a scan over the workgroup) followed, where rows of the table
 // change, by one wave per row.  A plan in several workgroups would need another launch for every scan, 2 to 3 us each, which is
-// what one workgroup takes for the counts of 16384 pages.
+// what one workgroup takes for the counts of 16384 pages.  Small calls (kSmallList entries of a table of kSmallRows rows, kSmallTable
+// table entries to change) keep what passes between threads in LDS and do the rows in the plan's launch.
 #include <climits>
 
 #include "lorc_device.h"
@@ -15,7 +16,8 @@
 namespace lorc {
 
 namespace {
-constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64, kPerThread = 16;
+constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64, kPerThread = 16, kStep = kPlanThreads * kPerThread;
+constexpr int kSmallList = kPlanThreads, kSmallRows = 4096, kSmallTable = 8192;
 
 __device__ __forceinline__ bool maps(int id, int n_pages) { return id >= 0 && id < n_pages; }
 // Values that other waves of the workgroup wrote through atomics are read past the vector cache.
@@ -66,13 +68,13 @@ __device__ __forceinline__ uint32_t free_mask(const int* refs, int first, int n_
 }
 
 // emit(k, page) for the free pages of rank k < want, in ascending order; returns how many free pages there are among those walked
-// (all of them where fewer than `want` exist).
+// (all of them where fewer than `want` exist).  first_mask: free_mask of the thread's first 16 pages, asked for early.
 template <typename F>
-__device__ __forceinline__ int each_free(const int* refs, int n_pages, int want, int* sums, F emit) {
+__device__ __forceinline__ int each_free(const int* refs, int n_pages, uint32_t first_mask, int want, int* sums, F emit) {
   int seen = 0;
-  for (int base = 0; base < n_pages && seen < want; base += kPlanThreads * kPerThread) {
+  for (int base = 0; base < n_pages && seen < want; base += kStep) {
     const int first = base + (int)threadIdx.x * kPerThread;
-    uint32_t mask = first < n_pages ? free_mask(refs, first, n_pages) : 0u;
+    uint32_t mask = base == 0 ? first_mask : first < n_pages ? free_mask(refs, first, n_pages) : 0u;
     int total;
     int rank = seen + block_exclusive(__popc(mask), sums, &total);
     while (mask != 0 && rank < want) {
@@ -82,6 +84,27 @@ __device__ __forceinline__ int each_free(const int* refs, int n_pages, int want,
     seen += total;
   }
   return seen;
+}
+__device__ __forceinline__ uint32_t first_free_mask(const int* refs, int n_pages) {
+  const int first = (int)threadIdx.x * kPerThread;
+  return first < n_pages ? free_mask(refs, first, n_pages) : 0u;
+}
+// Words that pass between the threads of a plan: in LDS, or in the workspace.
+template <bool LDS>
+__device__ __forceinline__ int get(const int* p) {
+  if constexpr (LDS) return *p;
+  return load_fresh(p);
+}
+template <bool LDS>
+__device__ __forceinline__ void put(int* p, int v) {
+  if constexpr (LDS) *p = v;
+  else store_fresh(p, v);
+}
+// Meets the other waves; what any of them put is there to get afterwards.  (Nothing else passes between the threads of a plan, so
+// that it needs no fence: one at device scope writes the caches back, 2 to 3 us each.)
+__device__ __forceinline__ void plan_barrier() {
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
 }
 }  // namespace
 
@@ -111,12 +134,29 @@ __global__ __launch_bounds__(256) void copy_pages_kernel(unsigned char* pool, si
 }
 
 // ------------------------------------------------------------------------------------------------ fork
-// Workspace: owner [n_seqs] (the lowest pair that names a row as its child), asks [n_seqs] (pairs that need a page, in order).
+// One wave: the child's row, and the counts of the pages that it shares.
+__device__ __forceinline__ void fork_row(const ForkParams& p, int parent, int child, int len, int fresh) {
+  const int whole = len / kPage, *from = p.block_table + (size_t)parent * p.max_pages;
+  int* to = p.block_table + (size_t)child * p.max_pages;
+  for (int e = threadIdx.x & 63; e < p.max_pages; e += 64) {
+    int id = e < whole ? from[e] : e == whole ? fresh : -1;
+    if (!maps(id, p.n_pages)) id = -1;
+    else if (e < whole) atomicAdd(p.page_refs + id, 1);
+    else p.page_refs[id] = 1;
+    to[e] = id;
+  }
+}
+
+// owner: the lowest pair that names a row as its child; asks: the pairs that need a page, in order.  ROWS (with SMALL): the rows
+// as well.
+template <bool SMALL, bool ROWS>
 __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(ForkParams p) {
-  __shared__ int sums[kPlanWaves];
+  __shared__ int sums[kPlanWaves], owner_lds[SMALL ? kSmallRows : 1], asks_lds[SMALL ? kSmallList : 1], fresh_lds[ROWS ? kSmallList : 1];
+  int* owner = SMALL ? owner_lds : p.owner;
+  int* asks = SMALL ? asks_lds : p.asks;
   const int tid = threadIdx.x;
-  for (int s = tid; s < p.n_seqs; s += kPlanThreads) store_fresh(p.owner + s, INT_MAX);
-  __syncthreads();
+  const uint32_t first_mask = first_free_mask(p.page_refs, p.n_pages);
+  for (int s = tid; s < p.n_seqs; s += kPlanThreads) put<SMALL>(owner + s, INT_MAX);
   const long most = (long)p.max_pages * kPage;
   auto named = [&](int i, int& parent, int& child, int& len) {
     parent = p.parents[i];
@@ -124,53 +164,54 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(ForkParams p) {
     len = p.lens[i];
     return parent >= 0 && parent < p.n_seqs && child >= 0 && child < p.n_seqs && parent != child && len >= 0 && len <= most;
   };
+  plan_barrier();
   for (int i = tid; i < p.n; i += kPlanThreads) {
     int parent, child, len;
-    if (named(i, parent, child, len)) atomicMin(p.owner + child, i);
+    if (named(i, parent, child, len)) atomicMin(owner + child, i);
   }
-  __syncthreads();
+  plan_barrier();
   int asked = 0;
   for (int base = 0; base < p.n; base += kPlanThreads) {
     const int i = base + tid;
     int parent, child, len, tail = -1;
     bool ok = i < p.n && named(i, parent, child, len);
-    ok = ok && load_fresh(p.owner + child) == i && load_fresh(p.owner + parent) == INT_MAX &&
-         !maps(p.block_table[(size_t)child * p.max_pages], p.n_pages);
-    if (ok && len % kPage != 0) tail = p.block_table[(size_t)parent * p.max_pages + len / kPage];
-    const bool asks = maps(tail, p.n_pages);
+    ok = ok && get<SMALL>(owner + child) == i && get<SMALL>(owner + parent) == INT_MAX;
+    if (ok) {
+      const int head = p.block_table[(size_t)child * p.max_pages];
+      if (len % kPage != 0) tail = p.block_table[(size_t)parent * p.max_pages + len / kPage];
+      ok = !maps(head, p.n_pages);
+    }
+    const bool tails = ok && maps(tail, p.n_pages);
     int total;
-    const int rank = asked + block_exclusive(asks ? 1 : 0, sums, &total);
+    const int rank = asked + block_exclusive(tails ? 1 : 0, sums, &total);
     asked += total;
-    if (asks) store_fresh(p.asks + rank, i);
+    if (tails) put<SMALL>(asks + rank, i);
     if (i < p.n) {
-      p.status[i] = !ok ? LORC_PAGES_REFUSED : asks ? LORC_PAGES_SHORT : LORC_PAGES_OK;  // (short until a page is found below)
-      p.copy_src[i] = asks ? tail : -1;
+      p.status[i] = !ok ? LORC_PAGES_REFUSED : tails ? LORC_PAGES_SHORT : LORC_PAGES_OK;  // (short until a page is found below)
+      p.copy_src[i] = tails ? tail : -1;
       p.copy_dst[i] = -1;
+      if constexpr (ROWS) fresh_lds[i] = !ok ? -3 : tails ? -2 : -1;  // refused, short, no page of its own
     }
   }
-  __syncthreads();
-  const int found = each_free(p.page_refs, p.n_pages, asked, sums, [&](int k, int page) {
-    const int i = load_fresh(p.asks + k);
+  plan_barrier();
+  const int found = each_free(p.page_refs, p.n_pages, first_mask, asked, sums, [&](int k, int page) {
+    const int i = get<SMALL>(asks + k);
     p.copy_dst[i] = page;
     p.status[i] = LORC_PAGES_OK;
+    if constexpr (ROWS) fresh_lds[i] = page;
   });
-  for (int k = found + tid; k < asked; k += kPlanThreads) p.copy_src[load_fresh(p.asks + k)] = -1;
+  for (int k = found + tid; k < asked; k += kPlanThreads) p.copy_src[get<SMALL>(asks + k)] = -1;
+  if constexpr (ROWS) {
+    plan_barrier();
+    for (int i = tid >> 6; i < p.n; i += kPlanWaves)
+      if (fresh_lds[i] >= -1) fork_row(p, p.parents[i], p.children[i], p.lens[i], fresh_lds[i]);
+  }
 }
 
-// One wave per pair: the child's row, and the counts of the pages that it shares.
 __global__ __launch_bounds__(256) void fork_rows_kernel(ForkParams p) {
-  const int i = blockIdx.x * 4 + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int i = blockIdx.x * 4 + (int)(threadIdx.x >> 6);
   if (i >= p.n || p.status[i] != LORC_PAGES_OK) return;
-  const int whole = p.lens[i] / kPage, fresh = p.copy_dst[i];
-  const int* from = p.block_table + (size_t)p.parents[i] * p.max_pages;
-  int* to = p.block_table + (size_t)p.children[i] * p.max_pages;
-  for (int e = lane; e < p.max_pages; e += 64) {
-    int id = e < whole ? from[e] : e == whole ? fresh : -1;
-    if (!maps(id, p.n_pages)) id = -1;
-    else if (e < whole) atomicAdd(p.page_refs + id, 1);
-    else p.page_refs[id] = 1;
-    to[e] = id;
-  }
+  fork_row(p, p.parents[i], p.children[i], p.lens[i], p.copy_dst[i]);
 }
 
 // ------------------------------------------------------------------------------------------------ free
@@ -189,24 +230,29 @@ __global__ __launch_bounds__(256) void free_rows_kernel(int* block_table, int n_
 }
 
 // ------------------------------------------------------------------------------------------------ compact
-// U pages are in use: the k-th lowest free page (below U) takes the contents of the k-th highest used one (at U or above).
+// U pages are in use: the k-th lowest free page (below U) takes the contents of the k-th highest used one (at U or above).  RENAME: the
+// table as well.
+template <bool RENAME>
 __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(CompactParams p) {
   __shared__ int sums[kPlanWaves];
   const int tid = threadIdx.x;
-  constexpr int kStep = kPlanThreads * kPerThread;
+  const uint32_t first_mask = first_free_mask(p.page_refs, p.n_pages);
+  auto mask_of = [&](int base) {
+    const int first = base + tid * kPerThread;
+    return base == 0 ? first_mask : first < p.n_pages ? free_mask(p.page_refs, first, p.n_pages) : 0u;
+  };
   int n_free = 0;
   for (int base = 0; base < p.n_pages; base += kStep) {
-    const int first = base + tid * kPerThread;
     int total;
-    block_exclusive(first < p.n_pages ? __popc(free_mask(p.page_refs, first, p.n_pages)) : 0, sums, &total);
+    block_exclusive(__popc(mask_of(base)), sums, &total);
     n_free += total;
   }
   const int used = p.n_pages - n_free;
   int holes = 0;  // free pages below `used`: as many as used pages from there on
   for (int base = 0; base < used; base += kStep) {
-    const int first = base + tid * kPerThread;
-    uint32_t mask = first < used ? free_mask(p.page_refs, first, p.n_pages) : 0u;
-    if (first < used && first + kPerThread > used) mask &= (1u << (used - first)) - 1u;
+    const int first = base + tid * kPerThread, n_here = used - first;
+    uint32_t mask = mask_of(base);
+    if (n_here < kPerThread) mask &= n_here <= 0 ? 0u : (1u << n_here) - 1u;
     int total;
     int rank = holes + block_exclusive(__popc(mask), sums, &total);
     for (uint32_t m = mask; m != 0; m &= m - 1, ++rank)
@@ -214,34 +260,36 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(CompactParam
     holes += total;
   }
   const int moves = holes < p.max_moves ? holes : p.max_moves;
-  __syncthreads();
   for (int k = moves + tid; k < p.max_moves; k += kPlanThreads) p.move_src[k] = p.move_dst[k] = -1;
-  for (int id = tid; id < used; id += kPlanThreads) p.page_map[id] = id;
+  for (int id = tid; id < p.n_pages; id += kPlanThreads) store_fresh(p.page_map + id, id);
   int rest = holes;  // used pages not yet walked
-  for (int base = used; base < p.n_pages; base += kStep) {
+  for (int base = used / kStep * kStep; base < p.n_pages; base += kStep) {
     const int first = base + tid * kPerThread;
-    int n_here = p.n_pages - first;
+    int n_here = p.n_pages - first, skip = used - first;  // pages [skip, n_here) of the thread's count
     n_here = n_here < 0 ? 0 : (n_here > kPerThread ? kPerThread : n_here);
-    const uint32_t all = (1u << n_here) - 1u;
-    uint32_t free_here = 0;
-    for (int u = 0; u < n_here; ++u) free_here |= (p.page_refs[first + u] <= 0 ? 1u : 0u) << u;
-    const uint32_t mask = all & ~free_here;
+    skip = skip < 0 ? 0 : (skip > n_here ? n_here : skip);
+    const uint32_t mask = ~mask_of(base) & ((1u << n_here) - 1u) & ~((1u << skip) - 1u);
     int total;
     int k = rest - 1 - block_exclusive(__popc(mask), sums, &total);  // rank from the top
-    for (int u = 0; u < n_here; ++u) {
-      int to = first + u;
-      if (mask >> u & 1u) {
-        if (k < moves) {
-          to = load_fresh(p.move_dst + k);
-          p.move_src[k] = first + u;
-          p.page_refs[to] = p.page_refs[first + u];
-          p.page_refs[first + u] = 0;
-        }
-        --k;
-      }
-      p.page_map[first + u] = to;
-    }
+    for (uint32_t m = mask; m != 0; m &= m - 1, --k)
+      if (k < moves) store_fresh(p.move_src + k, first + __ffs(m) - 1);
     rest -= total;
+  }
+  plan_barrier();
+  for (int k = tid; k < moves; k += kPlanThreads) {
+    const int from = load_fresh(p.move_src + k), to = load_fresh(p.move_dst + k);
+    p.page_refs[to] = p.page_refs[from];
+    p.page_refs[from] = 0;
+    store_fresh(p.page_map + from, to);
+  }
+  if constexpr (RENAME) {
+    plan_barrier();
+    for (int e = tid; e < p.n_seqs * p.max_pages; e += kPlanThreads) {
+      const int id = p.block_table[e];
+      if (!maps(id, p.n_pages)) continue;
+      const int to = load_fresh(p.page_map + id);
+      if (to != id) p.block_table[e] = to;
+    }
   }
 }
 
@@ -255,74 +303,105 @@ __global__ __launch_bounds__(256) void rename_pages_kernel(int* block_table, siz
 }
 
 // ------------------------------------------------------------------------------------------------ reserve
-// Workspace: owner [n_seqs] (the first place in the list that names a row), first [n_seqs] (rank of the row's first new page),
-// pages [n_pages] (free pages by rank).
+// Sixteen lanes: the row's unmapped entries below n_e take the pages of rank `rank` and on.  (Every lane of a wave calls it.)
+__device__ __forceinline__ void reserve_row(const ReserveParams& p, int s, int n_e, int rank, const int* pages) {
+  const int lane = threadIdx.x & 63, l16 = lane & 15;
+  int* row = p.block_table + (size_t)s * p.max_pages;
+  for (int e0 = 0; __any(e0 < n_e); e0 += 64) {
+    int id[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) id[u] = e0 + 16 * u + l16 < n_e ? row[e0 + 16 * u + l16] : 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const bool missing = e0 + 16 * u + l16 < n_e && !maps(id[u], p.n_pages);
+      const uint32_t who = (uint32_t)(__ballot(missing) >> (lane & 48)) & 0xffffu;
+      if (missing) {
+        const int page = pages[rank + __popc(who & ((1u << l16) - 1u))];
+        row[e0 + 16 * u + l16] = page;
+        p.page_refs[page] = 1;
+      }
+      rank += __popc(who);
+    }
+  }
+}
+
+// owner: the first place in the list that names a row; first: rank of the first new page, of a place in the list (SMALL) or of a row;
+// pages: the free pages by rank.  SMALL: the rows as well.
+template <bool SMALL>
 __global__ __launch_bounds__(kPlanThreads) void reserve_plan_kernel(ReserveParams p) {
-  __shared__ int sums[kPlanWaves];
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  for (int s = tid; s < p.n_seqs; s += kPlanThreads) store_fresh(p.owner + s, INT_MAX);
-  __syncthreads();
+  __shared__ int sums[kPlanWaves], owner_lds[SMALL ? kSmallRows : 1], first_lds[SMALL ? kSmallList : 1], pages_lds[SMALL ? kSmallTable : 1];
+  int* owner = SMALL ? owner_lds : p.owner;
+  int* pages = SMALL ? pages_lds : p.pages;
+  const int tid = threadIdx.x;
+  const uint32_t first_mask = first_free_mask(p.page_refs, p.n_pages);
+  for (int s = tid; s < p.n_seqs; s += kPlanThreads) put<SMALL>(owner + s, INT_MAX);
   const long most = (long)p.max_pages * kPage;
   auto named = [&](int i, int& s, int& len) {
     s = p.seqs[i];
     len = p.lens[i];
     return s >= 0 && s < p.n_seqs && len >= 0 && len <= most;
   };
+  auto first_of = [&](int i, int s) { return SMALL ? first_lds + i : p.first + s; };
+  plan_barrier();
   for (int i = tid; i < p.n; i += kPlanThreads) {
     int s, len;
-    if (named(i, s, len)) atomicMin(p.owner + s, i);
+    if (named(i, s, len)) atomicMin(owner + s, i);
   }
-  __syncthreads();
-  for (int i = w; i < p.n; i += kPlanWaves) {  // how many entries of the row map nothing yet
+  plan_barrier();
+  for (int i = tid >> 4; i < p.n; i += kPlanThreads / 16) {  // how many entries of the row map nothing yet: sixteen lanes per row
     int s, len;
-    if (!named(i, s, len) || load_fresh(p.owner + s) != i) continue;
-    const int n_e = (len + kPage - 1) / kPage;
-    const int* row = p.block_table + (size_t)s * p.max_pages;
+    const bool mine = named(i, s, len) && get<SMALL>(owner + s) == i;
+    const int n_e = mine ? (len + kPage - 1) / kPage : 0;
+    const int* row = p.block_table + (size_t)(mine ? s : 0) * p.max_pages;
     int missing = 0;
-    for (int e = lane; e < n_e; e += 64) missing += maps(row[e], p.n_pages) ? 0 : 1;
-    missing = wave_inclusive(missing);
-    if (lane == 63) store_fresh(p.first + s, missing);
+#pragma unroll 4
+    for (int e = tid & 15; e < n_e; e += 16) missing += maps(row[e], p.n_pages) ? 0 : 1;
+#pragma unroll
+    for (int step = 1; step < 16; step <<= 1) missing += __shfl_xor(missing, step, 16);
+    if (mine && (tid & 15) == 0) put<SMALL>(first_of(i, s), missing);
   }
-  __syncthreads();
+  plan_barrier();
   int asked = 0;
   for (int base = 0; base < p.n; base += kPlanThreads) {
     const int i = base + tid;
     int s, len;
-    const bool ok = i < p.n && named(i, s, len) && load_fresh(p.owner + s) == i;
-    const int missing = ok ? load_fresh(p.first + s) : 0;
+    const bool ok = i < p.n && named(i, s, len) && get<SMALL>(owner + s) == i;
+    const int missing = ok ? get<SMALL>(first_of(i, s)) : 0;
     int total;
     const int rank = asked + block_exclusive(missing, sums, &total);
     asked += total;
-    if (ok) store_fresh(p.first + s, rank);
+    if (ok) put<SMALL>(first_of(i, s), rank);
     if (i < p.n) p.status[i] = !ok ? LORC_PAGES_REFUSED : missing;  // (the count, until it is known whether they are there)
   }
-  __syncthreads();
-  const int found = each_free(p.page_refs, p.n_pages, asked, sums, [&](int k, int page) { p.pages[k] = page; });
+  plan_barrier();
+  const int found = each_free(p.page_refs, p.n_pages, first_mask, asked, sums, [&](int k, int page) { pages[k] = page; });
   for (int i = tid; i < p.n; i += kPlanThreads) {
     int s, len;
-    if (!named(i, s, len) || load_fresh(p.owner + s) != i) continue;
-    const int missing = p.status[i];
-    p.status[i] = missing == 0 || load_fresh(p.first + s) + missing <= found ? LORC_PAGES_OK : LORC_PAGES_SHORT;
+    const bool ok = named(i, s, len) && get<SMALL>(owner + s) == i;
+    if (!ok) {
+      if constexpr (SMALL) first_lds[i] = -1;
+      continue;
+    }
+    const int missing = p.status[i], rank = get<SMALL>(first_of(i, s));
+    const bool served = missing == 0 || rank + missing <= found;
+    p.status[i] = served ? LORC_PAGES_OK : LORC_PAGES_SHORT;
+    if constexpr (SMALL) first_lds[i] = served && missing > 0 ? rank : -1;
+  }
+  if constexpr (SMALL) {
+    plan_barrier();
+    for (int i0 = 0; i0 < p.n; i0 += kPlanThreads / 16) {
+      const int i = i0 + (tid >> 4), rank = i < p.n ? first_lds[i] : -1;
+      reserve_row(p, rank >= 0 ? p.seqs[i] : 0, rank >= 0 ? (p.lens[i] + kPage - 1) / kPage : 0, rank, pages);
+    }
   }
 }
 
+// Sixteen lanes per place in the list (a large call's `first` is the row's).
 __global__ __launch_bounds__(256) void reserve_rows_kernel(ReserveParams p) {
-  const int i = blockIdx.x * 4 + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (i >= p.n || p.status[i] != LORC_PAGES_OK) return;
-  const int s = p.seqs[i], n_e = (p.lens[i] + kPage - 1) / kPage;
-  int* row = p.block_table + (size_t)s * p.max_pages;
-  int rank = p.first[s];
-  for (int e0 = 0; e0 < n_e; e0 += 64) {
-    const int e = e0 + lane;
-    const bool missing = e < n_e && !maps(row[e], p.n_pages);
-    const uint64_t who = __ballot(missing);
-    if (missing) {
-      const int id = p.pages[rank + __popcll(who & ((1ull << lane) - 1ull))];
-      row[e] = id;
-      p.page_refs[id] = 1;
-    }
-    rank += __popcll(who);
-  }
+  const int i = blockIdx.x * 16 + (int)(threadIdx.x >> 4);
+  const bool served = i < p.n && p.status[i] == LORC_PAGES_OK;
+  const int s = served ? p.seqs[i] : 0;
+  reserve_row(p, s, served ? (p.lens[i] + kPage - 1) / kPage : 0, served ? p.first[s] : 0, p.pages);
 }
 
 // ------------------------------------------------------------------------------------------------ host
@@ -334,8 +413,11 @@ int launch_copy_pages(void* pool, size_t page_bytes, int n_pages, const int32_t*
 }
 
 int launch_fork(const ForkParams& p, hipStream_t s) {
-  if (int rc = launch_kernel(fork_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, p)) return rc;
-  return launch_kernel(fork_rows_kernel, dim3((p.n + 3) / 4), dim3(256), 0, s, p);
+  const bool small = p.n <= kSmallList && p.n_seqs <= kSmallRows, rows = small && (long)p.n * p.max_pages <= kSmallTable;
+  if (int rc = launch_kernel(rows ? fork_plan_kernel<true, true> : small ? fork_plan_kernel<true, false> : fork_plan_kernel<false, false>, dim3(1),
+                             dim3(kPlanThreads), 0, s, p))
+    return rc;
+  return rows ? LORC_OK : launch_kernel(fork_rows_kernel, dim3((p.n + 3) / 4), dim3(256), 0, s, p);
 }
 
 int launch_free(int32_t* block_table, int n_seqs, int max_pages, int32_t* page_refs, int n_pages, const int32_t* seqs, int n, hipStream_t s) {
@@ -343,15 +425,20 @@ int launch_free(int32_t* block_table, int n_seqs, int max_pages, int32_t* page_r
 }
 
 int launch_compact(const CompactParams& p, hipStream_t s) {
-  if (int rc = launch_kernel(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, p)) return rc;
   const size_t entries = (size_t)p.n_seqs * p.max_pages;
+  const bool rename = entries <= kSmallTable;
   if (entries > (size_t)0x7fffffff * 256) return LORC_EINVAL;
+  if (int rc = launch_kernel(rename ? compact_plan_kernel<true> : compact_plan_kernel<false>, dim3(1), dim3(kPlanThreads), 0, s, p)) return rc;
+  if (rename) return LORC_OK;
   return launch_kernel(rename_pages_kernel, dim3((uint32_t)((entries + 255) / 256)), dim3(256), 0, s, p.block_table, entries, p.page_map, p.n_pages);
 }
 
 int launch_reserve(const ReserveParams& p, hipStream_t s) {
-  if (int rc = launch_kernel(reserve_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, p)) return rc;
-  return launch_kernel(reserve_rows_kernel, dim3((p.n + 3) / 4), dim3(256), 0, s, p);
+  // (first is kept by place in the list only where the rows are done in the same launch)
+  const bool rows = p.n <= kSmallList && p.n_seqs <= kSmallRows && (long)p.n * p.max_pages <= kSmallTable;
+  if (int rc = launch_kernel(rows ? reserve_plan_kernel<true> : reserve_plan_kernel<false>, dim3(1), dim3(kPlanThreads), 0, s, p))
+    return rc;
+  return rows ? LORC_OK : launch_kernel(reserve_rows_kernel, dim3((p.n + 15) / 16), dim3(256), 0, s, p);
 }
 
 }  // namespace lorc
