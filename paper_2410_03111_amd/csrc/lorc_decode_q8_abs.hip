@@ -58,8 +58,14 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_absorbed_kernel(Dec
   if (tile_end > n_tiles) tile_end = n_tiles;
   const int nt = tile_end > tile_begin ? tile_end - tile_begin : 0;
   const uint32_t page_bytes = (uint32_t)p.page_elems * 2u;
+  const int* table = p.block_table + (size_t)seq * p.max_pages;
+  auto fetch_id = [&](int t) {  // (in bounds whatever the context is, so that it does not wait for it)
+    const int tile = tile_begin + t < p.max_pages ? tile_begin + t : p.max_pages - 1;
+    return table[tile];
+  };
+  const int id0 = fetch_id(0), id1 = fetch_id(1);
   for (int i = tid; i < nt; i += NT) {
-    const int id = p.block_table[(size_t)seq * p.max_pages + tile_begin + i];
+    const int id = table[tile_begin + i];
     ids[i] = id >= 0 && id < p.n_pages ? id : -1;
   }
   if (r_k < 128 * N) {  // the padding of the K tiles
@@ -72,14 +78,16 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_absorbed_kernel(Dec
   // scale bytes of both parts, by every wave, come with K: the softmax reference takes the values' scales
   const uint32_t lane16 = (uint32_t)lane * 16u;
   const int k_rows = r_k >> 5, k_blocks = 2 * k_rows, v_blocks = r_v >> 4;
-  auto rsrc_of = [&](int t) {
+  auto tile_id = [&](int t) {
     const int id = __builtin_amdgcn_readfirstlane(ids[t < nt ? t : 0]);
-    const bool ok = t < nt && id >= 0;
+    return t < nt ? id : -1;
+  };
+  auto rsrc_of = [&](int id) {
+    const bool ok = id >= 0;
     return dma_rsrc(reinterpret_cast<const unsigned char*>(p.cache) + (ok ? (size_t)id * page_bytes : 0), ok ? page_bytes : 0u);
   };
-  auto copy_k = [&](int t) {
-    const u32x4 r = rsrc_of(t);
-    const int buf = t & 1;
+  auto copy_k = [&](int id, int buf) {
+    const u32x4 r = rsrc_of(id);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       int b = w + NW * i;
@@ -90,9 +98,8 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_absorbed_kernel(Dec
     dma_256(r, uniform_u32(s_lds + (uint32_t)(buf * 512)), lane16 >> 2, uniform_u32((uint32_t)(64 * (r_k + r_v))));
     dma_256(r, uniform_u32(s_lds + (uint32_t)(buf * 512 + 256)), lane16 >> 2, uniform_u32((uint32_t)(64 * (r_k + r_v + gk))));
   };
-  auto copy_v = [&](int t) {
-    const u32x4 r = rsrc_of(t);
-    const int buf = t & 1;
+  auto copy_v = [&](int id, int buf) {
+    const u32x4 r = rsrc_of(id);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       int b = w + NW * i;
@@ -101,6 +108,16 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_absorbed_kernel(Dec
     }
   };
   constexpr int kKCopies = N + 2, kVCopies = N;
+  {
+    auto valid_id = [&](int id_raw, int t) {
+      const int id = __builtin_amdgcn_readfirstlane(id_raw);
+      return t < nt && id >= 0 && id < p.n_pages ? id : -1;
+    };
+    const int first = valid_id(id0, 0);
+    copy_k(first, 0);
+    copy_v(first, 0);
+    copy_k(valid_id(id1, 1), 1);
+  }
 
   // ---- the query: head 16 hb + n16, latents 128 g + 32 kg .. + 31, under one power of two per head and group
   const int pb16 = w & 3, hb = w >> 2;
@@ -162,9 +179,6 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_absorbed_kernel(Dec
 #pragma unroll
     for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
   __builtin_amdgcn_s_waitcnt(0);  // no load but the copies is waited for from here on
-  copy_k(0);
-  copy_v(0);
-  copy_k(1);
 
   const int pos = 16 * pb16 + n16;  // this lane's position of the page (scores)
   const unsigned char* k_src = kbuf + (pb16 >> 1) * (KB / 2) + kg * 1024 + (16 * (pb16 & 1) + n16) * 8;
@@ -176,7 +190,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_absorbed_kernel(Dec
   for (int t = 0; t < nt; ++t) {
     const int buf = t & 1, valid = ctx - (tile_begin + t) * T;
     dma_barrier<kVCopies + kKCopies>();  // this page's K has landed (younger: its V, the next K); every wave is through the previous V
-    copy_v(t + 1);
+    copy_v(tile_id(t + 1), buf ^ 1);
     // ---- scores
     int k_bytes = 0;
     uint32_t ub[N], top = 127 + kLeastExp;
@@ -210,7 +224,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_absorbed_kernel(Dec
       xm[(16 * hb + 4 * kg + j) * 4 + pb16] = mx;  // (sixteen lanes, the same value)
     }
     lds_barrier();  // every wave is through this page's K and scales
-    copy_k(t + 2);
+    copy_k(tile_id(t + 2), buf);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int h = 16 * hb + 4 * kg + j;
