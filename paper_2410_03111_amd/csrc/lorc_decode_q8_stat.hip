@@ -70,70 +70,30 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
   int* ids = reinterpret_cast<int*>(turns_tab + HALF);
   const uint32_t k_lds = (uint32_t)(uintptr_t)kbuf, v_lds = (uint32_t)(uintptr_t)vbuf, s_lds = (uint32_t)(uintptr_t)sbytes;
 
-  int ctx = p.ctx_len[seq];
-  ctx = ctx < 0 ? 0 : (ctx > p.max_ctx ? p.max_ctx : ctx);
+  // ---- set-up: everything that is asked of memory goes out at once, the page ids first
   const int tile_begin = split * p.tiles_per_split;
-  int tile_end = tile_begin + p.tiles_per_split;
-  const int n_tiles = (ctx + T - 1) / T;
-  if (tile_end > n_tiles) tile_end = n_tiles;
-  const int nt = tile_end > tile_begin ? tile_end - tile_begin : 0;
+  const int* table = p.block_table + (size_t)seq * p.max_pages;
+  const int id0 = table[tile_begin < p.max_pages ? tile_begin : p.max_pages - 1];
+  int ctx = p.ctx_len[seq];
   const int q_pos = p.q_pos[seq];
+  int my_id = -1;  // (the split has at most kQ8Tiles pages)
+  if (tid < p.tiles_per_split && tile_begin + tid < p.max_pages) my_id = table[tile_begin + tid];
   const uint32_t page_bytes = (uint32_t)p.page_elems * 2u;
-
-  for (int i = tid; i < nt; i += NT) {
-    const int id = p.block_table[(size_t)seq * p.max_pages + tile_begin + i];
-    ids[i] = id >= 0 && id < p.n_pages ? id : -1;
-  }
-  {  // what is read before it is written: K's padding, the V tile and the weights "before" the first tile
-    const u32x4 z = {0u, 0u, 0u, 0u};
-    if (r_k < 64 * NS)
-      for (int i = tid; i < 2 * NS * 4096 / 16; i += NT) reinterpret_cast<u32x4*>(kbuf)[i] = z;
-    for (int i = tid; i < 64 * r_v / 16; i += NT) reinterpret_cast<u32x4*>(vbuf + 64 * r_v)[i] = z;
-    for (int i = tid; i < 4 * 128; i += NT) reinterpret_cast<u32x4*>(pbuf)[i] = z;
-    for (int i = tid; i < HW * kStatQPitch; i += NT) qrot[i] = 0u;
-    if (tid < kStatMaxHeads) {
-      alpha[tid] = 1.f;
-      l_fin[tid] = 0.f;
-    }
-    if (tid < HALF) turns_tab[tid] = p.rope_tab[tid] * kInvTwoPi;
-  }
-  __builtin_amdgcn_s_waitcnt(0);
-  __syncthreads();
-
-  // ---- copies of a tile: blocks of 1 KiB, wave w moves w, w + 8, ...
-  const uint32_t lane16 = (uint32_t)lane * 16u;
-  const int k_rows = r_k >> 5, k_blocks = 2 * k_rows, v_blocks = r_v >> 4;
-  auto tile_id = [&](int t) {
-    const bool in = t < nt;
-    const int id = __builtin_amdgcn_readfirstlane(ids[in ? t : 0]);
-    return in ? id : -1;
-  };
-  auto rsrc_of = [&](int id) {
-    const bool ok = id >= 0;
-    return dma_rsrc(reinterpret_cast<const unsigned char*>(p.cache) + (ok ? (size_t)id * page_bytes : 0), ok ? page_bytes : 0u);
-  };
-  auto copy_k = [&](int id, int buf) {
-    const u32x4 r = rsrc_of(id);
-#pragma unroll
-    for (int i = 0; i < (4 * NS + NW - 1) / NW; ++i) {
-      const int b = w + NW * i, pb = b >= k_rows ? 1 : 0, c = b - pb * k_rows;
-      if (b < k_blocks) dma_1k(r, uniform_u32(k_lds + (uint32_t)(buf * NS * 4096 + pb * NS * 2048 + c * 1024)), lane16, uniform_u32((uint32_t)b * 1024u));
-    }
-    if (w == 0) dma_256(r, uniform_u32(s_lds + (uint32_t)(buf * kQ8ScaleBytes)), lane16 >> 2, uniform_u32((uint32_t)(64 * (r_k + r_v))));
-  };
-  auto copy_v = [&](int id, int buf) {
-    const u32x4 r = rsrc_of(id);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int b = w + NW * i;
-      if (b < v_blocks) dma_1k(r, uniform_u32(v_lds + (uint32_t)(buf * 64 * r_v + b * 1024)), lane16, uniform_u32((uint32_t)(64 * r_k + b * 1024)));
-    }
-    if (w == NW - 1) dma_256(r, uniform_u32(s_lds + (uint32_t)((2 + buf) * kQ8ScaleBytes)), lane16 >> 2, uniform_u32((uint32_t)(64 * (r_k + r_v + gk))));
-  };
-
-  // ---- what stays in registers
   const int kvh = w >> 2, wq = w & 3;
-  i32x8 fac[NS][2];
+  // softmax of head w (and w + 8); waves past the last head repeat it (same values to the same words)
+  int sm_h[PPH];
+  uint32_t q_raw[PPH];  // the head's coordinates lane and lane + 64, bf16
+  float m_run[PPH], l_run[PPH];
+#pragma unroll
+  for (int u = 0; u < PPH; ++u) {
+    sm_h[u] = w + 8 * u < n_heads ? w + 8 * u : n_heads - 1;
+    const uint16_t* src = p.q + ((size_t)seq * p.h_q + h0 + sm_h[u]) * HD + lane;
+    q_raw[u] = (uint32_t)src[0] | (uint32_t)src[HALF] << 16;
+    m_run[u] = kNegInfS;
+    l_run[u] = 0.f;
+  }
+  const double theta_lane = p.rope_tab[lane] * kInvTwoPi;
+  i32x8 fac[NS][2];  // the factor: see the head of this file
   int fac_scale[2];
   {
     const int n = p.h_kv * HD, steps = coded_steps(r_k);
@@ -153,6 +113,67 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
     fac_scale[0] = (int)sc[0];
     fac_scale[1] = (int)sc[1];
   }
+  ctx = ctx < 0 ? 0 : (ctx > p.max_ctx ? p.max_ctx : ctx);
+  int tile_end = tile_begin + p.tiles_per_split;
+  const int n_tiles = (ctx + T - 1) / T;
+  if (tile_end > n_tiles) tile_end = n_tiles;
+  const int nt = tile_end > tile_begin ? tile_end - tile_begin : 0;
+
+  // ---- copies of a tile: blocks of 1 KiB, wave w moves w, w + 8, ...
+  auto fresh_lane = [&]() {  // (rebuilt where it is used: no register is kept for what is derived from it)
+    int l = lane_id();
+    asm volatile("" : "+v"(l));
+    return l;
+  };
+  const int k_rows = r_k >> 5, k_blocks = 2 * k_rows, v_blocks = r_v >> 4;
+  auto tile_id = [&](int t) {
+    const bool in = t < nt;
+    const int id = __builtin_amdgcn_readfirstlane(ids[in ? t : 0]);
+    return in ? id : -1;
+  };
+  auto rsrc_of = [&](int id) {
+    const bool ok = id >= 0;
+    return dma_rsrc(reinterpret_cast<const unsigned char*>(p.cache) + (ok ? (size_t)id * page_bytes : 0), ok ? page_bytes : 0u);
+  };
+  auto copy_k = [&](int id, int buf) {
+    const u32x4 r = rsrc_of(id);
+    const uint32_t lane4 = 4u * (uint32_t)fresh_lane(), lane16 = 4u * lane4;
+#pragma unroll
+    for (int i = 0; i < (4 * NS + NW - 1) / NW; ++i) {
+      const int b = w + NW * i, pb = b >= k_rows ? 1 : 0, c = b - pb * k_rows;
+      if (b < k_blocks) dma_1k(r, uniform_u32(k_lds + (uint32_t)(buf * NS * 4096 + pb * NS * 2048 + c * 1024)), lane16, uniform_u32((uint32_t)b * 1024u));
+    }
+    if (w == 0) dma_256(r, uniform_u32(s_lds + (uint32_t)(buf * kQ8ScaleBytes)), lane4, uniform_u32((uint32_t)(64 * (r_k + r_v))));
+  };
+  auto copy_v = [&](int id, int buf) {
+    const u32x4 r = rsrc_of(id);
+    const uint32_t lane4 = 4u * (uint32_t)fresh_lane(), lane16 = 4u * lane4;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int b = w + NW * i;
+      if (b < v_blocks) dma_1k(r, uniform_u32(v_lds + (uint32_t)(buf * 64 * r_v + b * 1024)), lane16, uniform_u32((uint32_t)(64 * r_k + b * 1024)));
+    }
+    if (w == NW - 1) dma_256(r, uniform_u32(s_lds + (uint32_t)((2 + buf) * kQ8ScaleBytes)), lane4, uniform_u32((uint32_t)(64 * (r_k + r_v + gk))));
+  };
+  {  // what is read before it is written: K's padding, the V tile and the weights "before" the first tile
+    const u32x4 z = {0u, 0u, 0u, 0u};
+    if (r_k < 64 * NS) {
+      for (int i = tid; i < 2 * NS * 4096 / 16; i += NT) reinterpret_cast<u32x4*>(kbuf)[i] = z;
+      lds_barrier();  // (the first copies land beside it)
+    }
+    const int first = __builtin_amdgcn_readfirstlane(id0);
+    copy_k(nt > 0 && first >= 0 && first < p.n_pages ? first : -1, 0);
+    for (int i = tid; i < 64 * r_v / 16; i += NT) reinterpret_cast<u32x4*>(vbuf + 64 * r_v)[i] = z;
+    for (int i = tid; i < 4 * 128; i += NT) reinterpret_cast<u32x4*>(pbuf)[i] = z;
+    for (int i = tid; i < HW * kStatQPitch; i += NT) qrot[i] = 0u;
+    if (tid < kStatMaxHeads) {
+      alpha[tid] = 1.f;
+      l_fin[tid] = 0.f;
+    }
+    if (tid < HALF) turns_tab[tid] = theta_lane;
+    if (tid < kQ8Tiles) ids[tid] = my_id >= 0 && my_id < p.n_pages ? my_id : -1;
+  }
+  lds_barrier();
   f16x2 rot[2][8];  // (cos, sin) of the offset in the tile, position block b, the lane's eight frequencies
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
@@ -165,18 +186,6 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
       rot[b][j][1] = static_cast<_Float16>(__builtin_amdgcn_sinf(fr));
     }
   }
-  // softmax of head w (and w + 8); waves past the last head repeat it (same values to the same words)
-  int sm_h[PPH];
-  float qx[PPH], qy[PPH], m_run[PPH], l_run[PPH];
-#pragma unroll
-  for (int u = 0; u < PPH; ++u) {
-    sm_h[u] = w + 8 * u < n_heads ? w + 8 * u : n_heads - 1;
-    const uint16_t* src = p.q + ((size_t)seq * p.h_q + h0 + sm_h[u]) * HD + lane;
-    qx[u] = bf16_to_float(src[0]) * p.q_scale;
-    qy[u] = bf16_to_float(src[HALF]) * p.q_scale;
-    m_run[u] = kNegInfS;
-    l_run[u] = 0.f;
-  }
   f32x4s o[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) o[i] = f32x4s{0.f, 0.f, 0.f, 0.f};
@@ -184,7 +193,6 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
 #pragma unroll
   for (int j = 0; j < 16; ++j) acc[0][j] = acc[1][j] = zero16[j] = 0.f;
 
-  copy_k(tile_id(0), 0);
   __builtin_amdgcn_s_waitcnt(0);  // the factor's loads too: none of them may be waited for inside the loop
 
   // ---- pieces of the stream
@@ -204,38 +212,39 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
     if constexpr (NS > 6) v |= (uint32_t)at[192] << 24;
     return (int)v;
   };
-  auto rotate = [&](f16x8 (&kf)[2], auto b_c, auto part_c) {  // rows 4 part .. 4 part + 3 and their partners
+  auto rotate = [&](f16x8 (&kf)[2], auto b_c, auto part_c) {  // rows 2 part, 2 part + 1 (of eight) and their partners
     constexpr int b = decltype(b_c)::value, part = decltype(part_c)::value;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int j = 4 * part + i;
+    for (int i = 0; i < 2; ++i) {
+      const int j = 2 * part + i;
       uint32_t cs = __builtin_bit_cast(uint32_t, rot[b][j]);
       asm volatile("" : "+v"(cs));  // (else all of them are widened ahead of the loop, and spilled)
       const f16x2 h = __builtin_bit_cast(f16x2, cs);
       const float x = acc[b][j], y = acc[b][j + 8], c = (float)h[0], s = (float)h[1];
-      kf[part][2 * i] = static_cast<_Float16>(x * c - y * s);
-      kf[part][2 * i + 1] = static_cast<_Float16>(y * c + x * s);
+      kf[j >> 2][2 * (j & 3)] = static_cast<_Float16>(x * c - y * s);
+      kf[j >> 2][2 * (j & 3) + 1] = static_cast<_Float16>(y * c + x * s);
     }
   };
   const uint32_t* q_src = qrot + (size_t)(kvh * G + (l32 < G && kvh * G + l32 < n_heads ? l32 : 0)) * kStatQPitch + 16 * wq + 4 * hf;
   float* s_dst = sp + (size_t)((wq * 2 + kvh) * 8 + 4 * hf) * T + l32;  // (rows past the group: filed, not read)
-  auto score = [&](const f16x8 (&kf)[2], auto b_c) {
-    constexpr int b = decltype(b_c)::value;
-    f32x16 sa = mfma32_f16(__builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4*>(q_src)), kf[0], zero16);
-    sa = mfma32_f16(__builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4*>(q_src + 8)), kf[1], sa);
+  auto score = [&](f32x16& sa, const f16x8 (&kf)[2], auto part_c) {
+    constexpr int part = decltype(part_c)::value;
+    sa = mfma32_f16(__builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4*>(q_src + 8 * part)), kf[part], part ? sa : zero16);
+  };
+  auto score_store = [&](const f32x16& sa, auto b_c) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) s_dst[j * T + 32 * b] = sa[j];
+    for (int j = 0; j < 4; ++j) s_dst[j * T + 32 * decltype(b_c)::value] = sa[j];
   };
   struct Softmax {
     float a[4], s, mx, e;
     uint32_t ub[4];
   };
   auto softmax_load = [&](Softmax& sm, int u, int buf) {
-    const int h = sm_h[u];
-    const float* src = sp + (size_t)(h < G ? h : 8 + h - G) * T + lane;
+    const int h = sm_h[u], l = PPH == 2 ? fresh_lane() : lane;
+    const float* src = sp + (size_t)(h < G ? h : 8 + h - G) * T + l;
 #pragma unroll
     for (int q = 0; q < 4; ++q) sm.a[q] = src[q * kStatMaxHeads * T];
-    const unsigned char* at = sbytes + (2 + buf) * kQ8ScaleBytes + lane;
+    const unsigned char* at = sbytes + (2 + buf) * kQ8ScaleBytes + l;
 #pragma unroll
     for (int g = 0; g < 4; ++g) sm.ub[g] = at[g < gv ? 64 * g : 0];
   };
@@ -252,29 +261,42 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
     sm.mx = row_max_step<1>(sm.mx);
     sm.mx = row_max_step<2>(sm.mx);
     sm.mx = row_max_step<3>(sm.mx);
+  };
+  auto softmax_weight = [&](Softmax& sm, int u) {
     const float2 rows = row_pair(sm.mx);
     const float2 halves = half_pair(fmaxf(rows.x, rows.y));
-    sm.mx = fmaxf(halves.x, halves.y);
-  };
-  auto softmax_store = [&](Softmax& sm, int u) {
-    const float m_new = fmaxf(fmaxf(m_run[u], sm.mx), kNoWeight);
+    const float m_new = fmaxf(fmaxf(m_run[u], fmaxf(halves.x, halves.y)), kNoWeight);
     const float al = __builtin_amdgcn_exp2f(m_run[u] - m_new);
     m_run[u] = m_new;
-    const float e = __builtin_amdgcn_exp2f(sm.s - m_new);
-    l_run[u] = l_run[u] * al + e;
+    sm.e = __builtin_amdgcn_exp2f(sm.s - m_new);
+    l_run[u] = l_run[u] * al + sm.e;
     alpha[sm_h[u]] = al;
-    uint16_t* dst = pbuf + ((size_t)((lane >> 5) * 64 + sm_h[u] + 16 * ((lane & 31) >> 3)) * 8 + (lane & 7));
+  };
+  auto softmax_store = [&](const Softmax& sm, int u) {
+    const int l = PPH == 2 ? fresh_lane() : lane;
+    uint16_t* dst = pbuf + ((size_t)((l >> 5) * 64 + sm_h[u] + 16 * ((l & 31) >> 3)) * 8 + (l & 7));
 #pragma unroll
     for (int g = 0; g < 4; ++g)  // (groups past the rank: filed, not read)
-      dst[g * 1024] = f16_bits(__builtin_amdgcn_ldexpf(e, (int)sm.ub[g] - 127));
+      dst[g * 1024] = f16_bits(__builtin_amdgcn_ldexpf(sm.e, (int)sm.ub[g] - 127));
   };
-  auto query = [&](int u, int pos0) {
-    const double turns = (double)(q_pos - pos0) * turns_tab[lane];
-    const float fr = (float)(turns - rint(turns)), cs = __builtin_amdgcn_cosf(fr), sn = __builtin_amdgcn_sinf(fr);
-    f16x2 v;
-    v[0] = static_cast<_Float16>(qx[u] * cs - qy[u] * sn);
-    v[1] = static_cast<_Float16>(qy[u] * cs + qx[u] * sn);
-    qrot[(size_t)sm_h[u] * kStatQPitch + lane] = __builtin_bit_cast(uint32_t, v);
+  struct Query {
+    double turns;
+    float cs, sn;
+  };
+  auto query_angle = [&](Query& qr) {
+    const float fr = (float)(qr.turns - rint(qr.turns));
+    qr.cs = __builtin_amdgcn_cosf(fr) * p.q_scale;
+    qr.sn = __builtin_amdgcn_sinf(fr) * p.q_scale;
+  };
+  auto query_store = [&](const Query& qr) {
+#pragma unroll
+    for (int u = 0; u < PPH; ++u) {
+      const float x = __uint_as_float(q_raw[u] << 16), y = __uint_as_float(q_raw[u] & 0xffff0000u);
+      f16x2 v;
+      v[0] = static_cast<_Float16>(x * qr.cs - y * qr.sn);
+      v[1] = static_cast<_Float16>(y * qr.cs + x * qr.sn);
+      qrot[(size_t)sm_h[u] * kStatQPitch + lane] = __builtin_bit_cast(uint32_t, v);
+    }
   };
   // O += P' codes: wave w owns latents 64 w .. 64 w + 63; block (jb, b): latents 64 w + 32 jb + 2 n16 + b
   const int n16 = lane & 15, kg = lane >> 4;
@@ -284,32 +306,40 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
   const int wv = has_v ? w : 0, jb_off = has_v2 ? 4 * 512 : 0;
   const unsigned char* v_src = vbuf + (size_t)(wv * 8 + (kg >> 1)) * 512 + ((kg & 1) * 32 + 2 * n16) * 8;
   const uint16_t* p_src = pbuf + (size_t)(wv >> 1) * 1024 + lane * 8;
-  auto pv = [&](int buf, auto jb_c, int valid, bool ragged) {
-    constexpr int jb = decltype(jb_c)::value;
-    const f32x4s al = *reinterpret_cast<const f32x4s*>(alpha + 4 * kg);
-    o[2 * jb] *= al;
-    o[2 * jb + 1] *= al;
+  struct PV {
+    f32x4s al;
+    f16x8 pf[2];
+    u32x4 v[2];
+  };
+  auto pv_prep = [&](PV& x) {
+    x.al = *reinterpret_cast<const f32x4s*>(alpha + 4 * kg);
+    x.pf[0] = load_frag_f16(p_src);
+    x.pf[1] = load_frag_f16(p_src + 512);
+  };
+  auto pv_load = [&](PV& x, int buf, int jb, int valid, bool ragged) {
 #pragma unroll
     for (int ph = 0; ph < 2; ++ph) {
-      u32x4 v = *reinterpret_cast<const u32x4*>(v_src + buf * 64 * r_v + jb * jb_off + ph * 1024);
+      x.v[ph] = *reinterpret_cast<const u32x4*>(v_src + buf * 64 * r_v + jb * jb_off + ph * 1024);
       if (ragged) {  // slots past the context hold anything, NaN codes too
-        int nv = valid - 32 * ph - 8 * kg;
-        nv = nv < 0 ? 0 : (nv > 8 ? 8 : nv);
-        const uint64_t keep = nv == 8 ? ~0ull : (1ull << (8 * nv)) - 1ull;
-        v[0] &= (uint32_t)keep;
-        v[1] &= (uint32_t)(keep >> 32);
-        v[2] &= (uint32_t)keep;
-        v[3] &= (uint32_t)(keep >> 32);
+        const u32x2 lo = keep_bytes(u32x2{x.v[ph][0], x.v[ph][1]}, valid - 32 * ph - 8 * kg);
+        const u32x2 hi = keep_bytes(u32x2{x.v[ph][2], x.v[ph][3]}, valid - 32 * ph - 8 * kg);
+        x.v[ph] = u32x4{lo[0], lo[1], hi[0], hi[1]};
       }
-      const f16x8 pf = load_frag_f16(p_src + ph * 512);
-      o[2 * jb] = mfma16_f16(pf, codes_f16(u32x2{v[0], v[1]}), o[2 * jb]);
-      o[2 * jb + 1] = mfma16_f16(pf, codes_f16(u32x2{v[2], v[3]}), o[2 * jb + 1]);
     }
+  };
+  auto pv_mul = [&](const PV& x, auto i_c) {  // block i = 2 jb + b
+    constexpr int i = decltype(i_c)::value, b = i & 1;
+    o[i] *= x.al;
+    o[i] = mfma16_f16(x.pf[0], codes_f16(u32x2{x.v[0][2 * b], x.v[0][2 * b + 1]}), o[i]);
+    o[i] = mfma16_f16(x.pf[1], codes_f16(u32x2{x.v[1][2 * b], x.v[1][2 * b + 1]}), o[i]);
   };
   using I0 = std::integral_constant<int, 0>;
   using I1 = std::integral_constant<int, 1>;
-  // where the pieces sit in the stream (sixteenths of it)
-  auto at = [](int x) constexpr { return x * U / 16; };
+  using I2 = std::integral_constant<int, 2>;
+  using I3 = std::integral_constant<int, 3>;
+  // Where the pieces sit in the stream: behind the x-th of 32 products (two per unit).  A product occupies the matrix core for 64
+  // cycles and the next of the same wave waits for it, so a piece between them costs nothing while it is short.
+  auto at = [](int x) constexpr { return x * (2 * U) / 32; };
 
   int valid_prev = 0;  // the tile before the first one has no positions
   for (int t = 0; t < nt; ++t) {
@@ -321,35 +351,58 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
       copy_k(next, prev);
     }
     f16x8 kf[2];
+    f32x16 sa;
     Softmax sm[PPH];
+    Query qr;
+    PV pv;
     i32x8 c[2];
     c[0] = k_operand(buf, I0{});
     const int k_scale[2] = {k_scales(buf, 0), k_scales(buf, 1)};
-    static_for<U>([&](auto u_c) {
-      constexpr int u = decltype(u_c)::value, b = u / NS, s = u % NS;
-      if constexpr (u + 1 < U) c[(u + 1) % 2] = k_operand(buf, std::integral_constant<int, u + 1 < U ? u + 1 : 0>{});
+    static_for<2 * U>([&](auto x_c) {
+      constexpr int x = decltype(x_c)::value, u = x / 2, part = x % 2, b = u / NS, s = u % NS;
+      if constexpr (part == 0 && u + 1 < U) c[(u + 1) % 2] = k_operand(buf, std::integral_constant<int, u + 1 < U ? u + 1 : 0>{});
       __builtin_amdgcn_sched_barrier(0);
-      acc[b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fac[s][0], c[u % 2], s == 0 ? zero16 : acc[b], 0, 0, s & 3, fac_scale[s >> 2], s >> 1, k_scale[b]);
-      acc[b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fac[s][1], c[u % 2], acc[b], 0, 0, s & 3, fac_scale[s >> 2], s >> 1, k_scale[b]);
-      if constexpr (u == at(1)) rotate(kf, I1{}, I0{});
-      if constexpr (u == at(2)) rotate(kf, I1{}, I1{});
-      if constexpr (u == at(3)) score(kf, I1{});
-      if constexpr (u == at(4)) {
-        lds_barrier();  // the previous tile's scores are complete
-        static_for<PPH>([&](auto h) { softmax_load(sm[h], h, prev); });
-      }
-      if constexpr (u == at(5)) static_for<PPH>([&](auto h) { softmax_max(sm[h], valid_prev); });
-      if constexpr (u == at(6)) static_for<PPH>([&](auto h) { softmax_rows(sm[h]); });
-      if constexpr (u == at(8)) static_for<PPH>([&](auto h) { softmax_store(sm[h], h); });
-      if constexpr (u == at(9)) static_for<PPH>([&](auto h) { query(h, pos0); });
-      if constexpr (u == at(11)) {
-        lds_barrier();  // its weights and this tile's queries too
-        pv(prev, I0{}, T, false);
-      }
-      if constexpr (u == at(12)) pv(prev, I1{}, T, false);
-      if constexpr (u == at(13)) rotate(kf, I0{}, I0{});
-      if constexpr (u == at(14)) rotate(kf, I0{}, I1{});
-      if constexpr (u == at(15)) score(kf, I0{});
+      acc[b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fac[s][part], c[u % 2], s == 0 && part == 0 ? zero16 : acc[b], 0, 0, s & 3,
+                                                               fac_scale[s >> 2], s >> 1, k_scale[b]);
+      // -- the previous tile's second position block
+      if constexpr (x == at(0)) rotate(kf, I1{}, I0{});
+      if constexpr (x == at(1)) rotate(kf, I1{}, I1{});
+      if constexpr (x == at(2)) rotate(kf, I1{}, I2{});
+      if constexpr (x == at(3)) rotate(kf, I1{}, I3{});
+      if constexpr (x == at(4)) score(sa, kf, I0{});
+      if constexpr (x == at(5)) score(sa, kf, I1{});
+      if constexpr (x == at(7)) score_store(sa, I1{});
+      if constexpr (x == at(8)) lds_barrier();  // its scores are complete
+      // -- its softmax, a head after the other
+      static_for<PPH>([&](auto h_c) {
+        constexpr int h = decltype(h_c)::value, x0 = 8 + 4 * h;
+        if constexpr (x == at(x0)) softmax_load(sm[h], h, prev);
+        if constexpr (x == at(x0 + 1)) softmax_max(sm[h], valid_prev);
+        if constexpr (x == at(x0 + 2)) softmax_rows(sm[h]);
+        if constexpr (x == at(x0 + 3)) softmax_weight(sm[h], h);
+        if constexpr (x == at(x0 + 4)) softmax_store(sm[h], h);
+      });
+      // -- this tile's queries
+      if constexpr (x == at(14)) qr.turns = (double)(q_pos - pos0) * turns_tab[lane];
+      if constexpr (x == at(15)) query_angle(qr);
+      if constexpr (x == at(17)) query_store(qr);
+      if constexpr (x == at(18)) lds_barrier();  // weights and queries are complete
+      // -- the previous tile's P' codes
+      if constexpr (x == at(18)) pv_prep(pv);
+      if constexpr (x == at(18)) pv_load(pv, prev, 0, T, false);
+      if constexpr (x == at(19)) pv_mul(pv, I0{});
+      if constexpr (x == at(20)) pv_mul(pv, I1{});
+      if constexpr (x == at(21)) pv_load(pv, prev, 1, T, false);
+      if constexpr (x == at(22)) pv_mul(pv, I2{});
+      if constexpr (x == at(23)) pv_mul(pv, I3{});
+      // -- this tile's first position block
+      if constexpr (x == at(24)) rotate(kf, I0{}, I0{});
+      if constexpr (x == at(25)) rotate(kf, I0{}, I1{});
+      if constexpr (x == at(26)) rotate(kf, I0{}, I2{});
+      if constexpr (x == at(27)) rotate(kf, I0{}, I3{});
+      if constexpr (x == at(28)) score(sa, kf, I0{});
+      if constexpr (x == at(29)) score(sa, kf, I1{});
+      if constexpr (x == at(31)) score_store(sa, I0{});
       __builtin_amdgcn_sched_barrier(0);
     });
     valid_prev = ctx - pos0 < T ? ctx - pos0 : T;
@@ -358,21 +411,33 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
   if (nt > 0) {  // the last tile's second half
     const int prev = (nt - 1) & 1;
     f16x8 kf[2];
+    f32x16 sa;
     Softmax sm[PPH];
+    PV pv;
     rotate(kf, I1{}, I0{});
     rotate(kf, I1{}, I1{});
-    score(kf, I1{});
+    rotate(kf, I1{}, I2{});
+    rotate(kf, I1{}, I3{});
+    score(sa, kf, I0{});
+    score(sa, kf, I1{});
+    score_store(sa, I1{});
     lds_barrier();
 #pragma unroll
     for (int h = 0; h < PPH; ++h) {
       softmax_load(sm[h], h, prev);
       softmax_max(sm[h], valid_prev);
       softmax_rows(sm[h]);
+      softmax_weight(sm[h], h);
       softmax_store(sm[h], h);
     }
     dma_barrier<0>();  // weights visible; the V codes have landed
-    pv(prev, I0{}, valid_prev, valid_prev < T);
-    pv(prev, I1{}, valid_prev, valid_prev < T);
+    pv_prep(pv);
+    pv_load(pv, prev, 0, valid_prev, valid_prev < T);
+    pv_mul(pv, I0{});
+    pv_mul(pv, I1{});
+    pv_load(pv, prev, 1, valid_prev, valid_prev < T);
+    pv_mul(pv, I2{});
+    pv_mul(pv, I3{});
   }
 
   // ---- partials: every copy has to land before its memory is used again
