@@ -150,7 +150,7 @@ extern "C" {
 
 size_t lorc_packed_bytes(const lorc_layer_desc* desc) {
   if (!desc || check_desc(*desc) != LORC_OK) return 0;
-  return packed_total_elems(desc->d_model, desc->rank_k, desc->rank_v, desc->n_kv_heads * desc->head_dim) * 2;
+  return packed_total_elems(desc->d_model, desc->rank_k, desc->rank_v, desc->n_kv_heads * desc->head_dim, desc->head_dim) * 2;
 }
 
 int lorc_pack_factors(const lorc_layer_desc* desc, const void* A_k, const void* A_v, const void* B_k,

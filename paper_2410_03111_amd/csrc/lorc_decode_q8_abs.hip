@@ -119,16 +119,17 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_absorbed_kernel(Dec
     copy_k(valid_id(id1, 1), 1);
   }
 
-  // ---- the query: head 16 hb + n16, latents 128 g + 32 kg .. + 31, under one power of two per head and group
+  // ---- the query: head 16 hb + n16, latents 128 g + 32 kg .. + 31, under one power of two per head and group.  The four waves of a head
+  // block make a group each and hand it round through the V buffer that is not in use yet.
   const int pb16 = w & 3, hb = w >> 2;
   i32x8 qa[N][2];
   int q_bytes = 0;
   {
-    const int h = 16 * hb + n16;
-    const uint16_t* row = p.q + ((size_t)seq * p.h_q + h0 + (h < nh ? h : 0)) * r_k;
-#pragma unroll
-    for (int g = 0; g < N; ++g) {
-      const int j0 = 128 * g + 32 * kg;
+    unsigned char* shared = vbuf + VB;
+    int* byte_of = reinterpret_cast<int*>(xm);  // [2 head blocks][4 groups][16 heads]
+    const int h = 16 * hb + n16, g = pb16, j0 = 128 * g + 32 * kg;
+    if (g < N) {
+      const uint16_t* row = p.q + ((size_t)seq * p.h_q + h0 + (h < nh ? h : 0)) * r_k;
       const bool real = h < nh && j0 < r_k;  // (ranks are multiples of 32)
       u32x4 v[4];
 #pragma unroll
@@ -153,18 +154,32 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_absorbed_kernel(Dec
       }
       const int byte = scale_byte(most);
       const float inv = inverse_scale(byte);
-      q_bytes |= byte << (8 * g);
+      if (kg == 0) byte_of[(hb * 4 + g) * 16 + n16] = byte;
+      int hi[8], lo[8];
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           const uint32_t x = v[i][2 * c], y = v[i][2 * c + 1];
-          int hi, lo;
           code_pair(__uint_as_float(x << 16) * inv, __uint_as_float(x & 0xffff0000u) * inv, __uint_as_float(y << 16) * inv,
-                    __uint_as_float(y & 0xffff0000u) * inv, hi, lo);
-          qa[g][0][2 * i + c] = hi;
-          qa[g][1][2 * i + c] = lo;
+                    __uint_as_float(y & 0xffff0000u) * inv, hi[2 * i + c], lo[2 * i + c]);
         }
+      u32x4* dst = reinterpret_cast<u32x4*>(shared + (size_t)(hb * N + g) * 4096) + lane;
+      dst[0] = u32x4{(uint32_t)hi[0], (uint32_t)hi[1], (uint32_t)hi[2], (uint32_t)hi[3]};
+      dst[64] = u32x4{(uint32_t)hi[4], (uint32_t)hi[5], (uint32_t)hi[6], (uint32_t)hi[7]};
+      dst[128] = u32x4{(uint32_t)lo[0], (uint32_t)lo[1], (uint32_t)lo[2], (uint32_t)lo[3]};
+      dst[192] = u32x4{(uint32_t)lo[4], (uint32_t)lo[5], (uint32_t)lo[6], (uint32_t)lo[7]};
+    }
+    lds_barrier();
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const u32x4* src = reinterpret_cast<const u32x4*>(shared + (size_t)(hb * N + u) * 4096) + lane;
+#pragma unroll
+      for (int part = 0; part < 2; ++part) {
+        const u32x4 a = src[128 * part], b = src[128 * part + 64];
+        qa[u][part] = i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+      }
+      q_bytes |= byte_of[(hb * 4 + u) * 16 + n16] << (8 * u);
     }
   }
   float m_run[4], l_run[4];  // of heads 16 hb + 4 kg + j: reference, and this lane's share of the sum

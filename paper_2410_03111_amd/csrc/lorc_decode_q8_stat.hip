@@ -96,20 +96,20 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
   i32x8 fac[NS][2];  // the factor: see the head of this file
   int fac_scale[2];
   {
-    const int n = p.h_kv * HD, steps = coded_steps(r_k);
-    const int col = (2 * hp + kvh) * HD + 16 * wq + l32 + (l32 < 16 ? 0 : HALF - 16);
+    const int n = p.h_kv * HD, steps = coded_steps(HD, r_k), block = (2 * hp + kvh) * 4 + wq;
     const __amdgpu_buffer_rsrc_t r = make_rsrc(p.coded, (uint32_t)steps * n * 128u + (uint32_t)n * 8u);
-    const bool real = col < n;  // (the last pair of an odd number of heads)
+    const bool real = 2 * hp + kvh < p.h_kv;  // (the last pair of an odd number of heads)
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const uint32_t at = real && s < steps ? (uint32_t)(s * n + col) * 128u + (uint32_t)hf * 64u + 32u * u : 0xfffffff0u;  // past the end: zeros
+        // (past the end: zeros; in the lane offset, which is what the bound is compared with)
+        const uint32_t at = real && s < steps ? (uint32_t)((block * steps + s) * 2 + u) * 2048u + lane * 16u : 0x7fff0000u;
         const u32x4 a = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0));
-        const u32x4 b = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at == 0xfffffff0u ? at : at + 16u, 0, 0));
+        const u32x4 b = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at + 1024u, 0, 0));
         fac[s][u] = i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
       }
-    const u32x2 sc = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, real ? (uint32_t)steps * n * 128u + (uint32_t)col * 8u : 0xfffffff0u, 0, 0));
+    const u32x2 sc = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, real ? (uint32_t)steps * n * 128u + (uint32_t)block * 256u + l32 * 8u : 0x7fff0000u, 0, 0));
     fac_scale[0] = (int)sc[0];
     fac_scale[1] = (int)sc[1];
   }
@@ -489,7 +489,7 @@ Q8StatKernel q8_stat_kernel(int ns) {
     default: return decode_q8_stationary_kernel<8, PPH>;
   }
 }
-int q8_stat_ns(int r_k) { return r_k <= 128 ? 2 : coded_steps(r_k); }
+int q8_stat_ns(int r_k) { return r_k <= 128 ? 2 : coded_steps(128, r_k); }
 }  // namespace
 
 bool q8_stationary_shape_ok(const lorc_layer_desc& d) {
