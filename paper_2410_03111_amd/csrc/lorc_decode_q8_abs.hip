@@ -64,6 +64,20 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_absorbed_kernel(Dec
     return table[tile];
   };
   const int id0 = fetch_id(0), id1 = fetch_id(1);
+  // this wave's share of the query, see below
+  const int pb16 = w & 3, hb = w >> 2;
+  u32x4 qv[4];
+  {
+    const int h = 16 * hb + n16, j0 = 128 * pb16 + 32 * kg;
+    const bool real = h < nh && j0 < r_k;  // (ranks are multiples of 32)
+    const uint16_t* row = p.q + ((size_t)seq * p.h_q + h0 + (h < nh ? h : 0)) * r_k + (real ? j0 : 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      qv[i] = *reinterpret_cast<const u32x4*>(row + 8 * i);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) qv[i][c] = real ? qv[i][c] : 0u;
+    }
+  }
   for (int i = tid; i < nt; i += NT) {
     const int id = table[tile_begin + i];
     ids[i] = id >= 0 && id < p.n_pages ? id : -1;
@@ -109,6 +123,8 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_absorbed_kernel(Dec
   };
   constexpr int kKCopies = N + 2, kVCopies = N;
   {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(qv[i]));  // here, not behind the copies: the counter of loads is one for both
     auto valid_id = [&](int id_raw, int t) {
       const int id = __builtin_amdgcn_readfirstlane(id_raw);
       return t < nt && id >= 0 && id < p.n_pages ? id : -1;
@@ -121,29 +137,19 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_absorbed_kernel(Dec
 
   // ---- the query: head 16 hb + n16, latents 128 g + 32 kg .. + 31, under one power of two per head and group.  The four waves of a head
   // block make a group each and hand it round through the V buffer that is not in use yet.
-  const int pb16 = w & 3, hb = w >> 2;
   i32x8 qa[N][2];
   int q_bytes = 0;
   {
     unsigned char* shared = vbuf + VB;
     int* byte_of = reinterpret_cast<int*>(xm);  // [2 head blocks][4 groups][16 heads]
-    const int h = 16 * hb + n16, g = pb16, j0 = 128 * g + 32 * kg;
+    const int g = pb16;
     if (g < N) {
-      const uint16_t* row = p.q + ((size_t)seq * p.h_q + h0 + (h < nh ? h : 0)) * r_k;
-      const bool real = h < nh && j0 < r_k;  // (ranks are multiples of 32)
-      u32x4 v[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[i] = *reinterpret_cast<const u32x4*>(row + (real ? j0 : 0) + 8 * i);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) v[i][c] = real ? v[i][c] : 0u;
-      }
       uint32_t most = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          const uint32_t a = magnitude(v[i][c] & 0xffffu), b = magnitude(v[i][c] >> 16);
+          const uint32_t a = magnitude(qv[i][c] & 0xffffu), b = magnitude(qv[i][c] >> 16);
           most = most > a ? most : a;
           most = most > b ? most : b;
         }
@@ -160,7 +166,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_absorbed_kernel(Dec
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          const uint32_t x = v[i][2 * c], y = v[i][2 * c + 1];
+          const uint32_t x = qv[i][2 * c], y = qv[i][2 * c + 1];
           code_pair(__uint_as_float(x << 16) * inv, __uint_as_float(x & 0xffff0000u) * inv, __uint_as_float(y << 16) * inv,
                     __uint_as_float(y & 0xffff0000u) * inv, hi[2 * i + c], lo[2 * i + c]);
         }
@@ -293,16 +299,21 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_absorbed_kernel(Dec
     p.part_ml[(row0 + tid) * 2] = nt > 0 ? m_fin[tid] : kNegInfS;
     p.part_ml[(row0 + tid) * 2 + 1] = l_fin[tid];
   }
+  // rows through LDS, so that memory sees 16 bytes per lane: two bytes per lane took 4.4 us
+  const int pitch = r_v * 2 + 16;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    if (has_v[i]) {
+  for (int j = 0; j < 16; ++j) {
+    const int h = acc_row(j, hf);
+    const float l = l_fin[h], inv = l > 0.f ? __builtin_amdgcn_rcpf(l) : l == 0.f ? 0.f : l;
 #pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        const int h = acc_row(j, hf);
-        const float l = l_fin[h], inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
-        if (h < nh) p.part_o[(row0 + h) * r_v + 64 * w + 32 * i + l32] = f16_bits(o[i][j] * inv);
-      }
-    }
+    for (int i = 0; i < 2; ++i)
+      if (has_v[i]) *reinterpret_cast<uint16_t*>(smem + (size_t)h * pitch + (64 * w + 32 * i + l32) * 2) = f16_bits(o[i][j] * inv);
+  }
+  __syncthreads();
+  const int per_row = r_v >> 3;
+  for (int c = tid; c < nh * per_row; c += NT) {
+    const int h = c / per_row, cc = c - h * per_row;
+    *reinterpret_cast<u32x4*>(p.part_o + (row0 + h) * r_v + cc * 8) = *reinterpret_cast<const u32x4*>(smem + (size_t)h * pitch + cc * 16);
   }
 }
 
