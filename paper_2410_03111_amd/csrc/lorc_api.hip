@@ -39,6 +39,7 @@ int device_ready(int* n_cus) {
     if (int rc = set_kernel_attributes_decode_q8()) return rc;
     if (int rc = set_kernel_attributes_decode_q8_stationary()) return rc;
     if (int rc = set_kernel_attributes_decode_q8_absorbed()) return rc;
+    if (int rc = set_kernel_attributes_decode_q8_wide()) return rc;
     void* sp = nullptr;
     if (hipGetSymbolAddress(&sp, HIP_SYMBOL(scratch)) != hipSuccess || sp == nullptr) return LORC_EHIP;
     g_scratch_ptr[dev] = sp;

@@ -77,7 +77,10 @@ __global__ __launch_bounds__(256) void pack_codes_kernel(const uint16_t* __restr
     dst[at] = (uint32_t)hi;
     dst[512 + at] = (uint32_t)lo;
   }
-  coded[(size_t)steps * n * 128 + (size_t)(coded_block(c) * 32 + coded_row(c)) * 8 + s] = (unsigned char)byte;
+  unsigned char* bytes = coded + (size_t)steps * n * 128 + (size_t)(coded_block(c) * 32 + coded_row(c)) * kCodedMaxSteps;
+  bytes[s] = (unsigned char)byte;
+  if (s == 0)  // runs past the rank multiply zeros: by anything but NaN (255)
+    for (int u = steps; u < kCodedMaxSteps; ++u) bytes[u] = 127;
 }
 
 // ------------------------------------------------------------------------------------------------ append

@@ -413,13 +413,28 @@ DecodePlan make_q8_plan(const lorc_layer_desc& d, Q8Form form, int b, int max_ct
   pl.tile = kPage;
   int n_tiles = (max_ctx + kPage - 1) / kPage;
   if (n_tiles < 1) n_tiles = 1;
-  const bool stationary = form == Q8Form::kRotary && q8_stationary_shape_ok(d), absorbed = form == Q8Form::kAbsorbed && q8_absorbed_shape_ok(d);
-  const long units = form == Q8Form::kAbsorbed ? (d.n_q_heads + 31) / 32 : form == Q8Form::kPlain ? (d.n_kv_heads + 3) / 4 :
-                     stationary ? (d.n_kv_heads + 1) / 2 : d.n_kv_heads;
-  pl.stationary = stationary || absorbed;
-  const int most = stationary ? q8_stationary_max_tiles() : absorbed ? q8_absorbed_max_tiles() : n_tiles;
+  // units: workgroups per (sequence, split); per_cu: those that share a compute unit; most: pages that a split walks at most
+  long units, per_cu = 1, most = n_tiles;
+  if (form == Q8Form::kPlain) {
+    units = (d.n_kv_heads * ((d.n_q_heads / d.n_kv_heads + 15) / 16) + 3) / 4;
+    per_cu = 2;
+  } else if (form == Q8Form::kAbsorbed) {
+    units = (d.n_q_heads + 31) / 32;
+    pl.stationary = q8_absorbed_shape_ok(d);
+    if (pl.stationary) most = q8_absorbed_max_tiles();
+  } else if (q8_stationary_shape_ok(d)) {
+    units = (d.n_kv_heads + 1) / 2;
+    pl.stationary = 1;
+    most = q8_stationary_max_tiles();
+  } else if (q8_wide_shape_ok(d)) {
+    units = d.n_kv_heads * ((d.n_q_heads / d.n_kv_heads + 15) / 16);
+    pl.stationary = 2;
+    most = q8_wide_max_tiles();
+  } else {
+    units = d.n_kv_heads;
+  }
   const long least = (n_tiles + most - 1) / most;
-  long ns = ((stationary || absorbed ? 1L : 2L) * (n_cus > 0 ? n_cus : 256) + b * units - 1) / (b * units);
+  long ns = (per_cu * (n_cus > 0 ? n_cus : 256) + b * units - 1) / (b * units);
   if (ns > 64) ns = 64;
   if (ns > max_splits) ns = max_splits;
   if (ns < least) ns = least;
@@ -464,7 +479,10 @@ int launch_decode_q8(const lorc_layer_desc& d, Q8Form form, const DecodeParams& 
     return launch_decode_merge(p, true, s);
   }
   if (plan.stationary) {
-    if (int rc = form == Q8Form::kAbsorbed ? launch_decode_q8_absorbed(p, s) : launch_decode_q8_stationary(p, s)) return rc;
+    if (int rc = form == Q8Form::kAbsorbed ? launch_decode_q8_absorbed(p, s)
+                 : plan.stationary == 2    ? launch_decode_q8_wide(p, s)
+                                           : launch_decode_q8_stationary(p, s))
+      return rc;
     return launch_decode_merge(p, false, s);
   }
   const size_t lds = q8_lds_bytes(d);

@@ -97,7 +97,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
   int fac_scale[2];
   {
     const int n = p.h_kv * HD, steps = coded_steps(HD, r_k), block = (2 * hp + kvh) * 4 + wq;
-    const __amdgpu_buffer_rsrc_t r = make_rsrc(p.coded, (uint32_t)steps * n * 128u + (uint32_t)n * 8u);
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(p.coded, (uint32_t)(steps * 128 + kCodedMaxSteps) * (uint32_t)n);
     const bool real = 2 * hp + kvh < p.h_kv;  // (the last pair of an odd number of heads)
 #pragma unroll
     for (int s = 0; s < NS; ++s)
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
         const u32x4 b = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at + 1024u, 0, 0));
         fac[s][u] = i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
       }
-    const u32x2 sc = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, real ? (uint32_t)steps * n * 128u + (uint32_t)block * 256u + l32 * 8u : 0x7fff0000u, 0, 0));
+    const u32x2 sc = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, real ? (uint32_t)steps * n * 128u + (uint32_t)(block * 32 + l32) * (uint32_t)kCodedMaxSteps : 0x7fff0000u, 0, 0));
     fac_scale[0] = (int)sc[0];
     fac_scale[1] = (int)sc[1];
   }
@@ -493,7 +493,7 @@ int q8_stat_ns(int r_k) { return r_k <= 128 ? 2 : coded_steps(128, r_k); }
 }  // namespace
 
 bool q8_stationary_shape_ok(const lorc_layer_desc& d) {
-  return d.head_dim == 128 && d.n_q_heads / d.n_kv_heads <= kStatMaxHeads / 2 && d.rank_k <= kCodedMaxRank && d.rank_v <= 512;
+  return d.head_dim == 128 && d.n_q_heads / d.n_kv_heads <= kStatMaxHeads / 2 && d.rank_k <= 512 && d.rank_v <= 512;
 }
 
 int q8_stationary_max_tiles() { return kQ8Tiles; }

@@ -46,7 +46,8 @@ struct AppendParams {
 struct DecodePlan {
   int tile;             // positions per tile (64 or 128)
   int occupancy;        // workgroups meant to share a CU (1 or 2)
-  int stationary;       // the split kernels with the key factor held in registers: 1 lorc_decode_stat.hip, 2 lorc_decode_stat768.hip
+  int stationary;       // the split kernels with the key factor held in registers: 1 lorc_decode_stat.hip, 2 lorc_decode_stat768.hip;
+                        // 8-bit pages: 1 lorc_decode_q8_stat.hip (_abs.hip where the query is absorbed), 2 lorc_decode_q8_wide.hip
   int wide;             // lorc_decode_wide.hip: 1 ranks above 1024, 2 uncompressed layer, 3 absorbed query (scores, values, merge;
                         // uncompressed layers of eight KV heads or a multiple: one pass, merge)
   int score_stride;     // wide: positions per score row (max_ctx rounded up to whole tiles)
@@ -190,6 +191,11 @@ bool q8_stationary_shape_ok(const lorc_layer_desc& d);
 int q8_stationary_max_tiles();  // pages that a split of it walks at most
 int set_kernel_attributes_decode_q8_stationary();
 int launch_decode_q8_stationary(const DecodeParams& p, hipStream_t s);
+// The same for ranks up to 1024 and any group (lorc_decode_q8_wide.hip).
+bool q8_wide_shape_ok(const lorc_layer_desc& d);
+int q8_wide_max_tiles();
+int set_kernel_attributes_decode_q8_wide();
+int launch_decode_q8_wide(const DecodeParams& p, hipStream_t s);
 // Absorbed form up to rank 512 (lorc_decode_q8_abs.hip).
 bool q8_absorbed_shape_ok(const lorc_layer_desc& d);
 int q8_absorbed_max_tiles();

@@ -147,6 +147,12 @@ SHAPES = {
     "rotary groups of 1": dict(form="rotary", h_q=16, h_kv=16, r_k=192, r_v=512),
     "rotary rank 1024": dict(form="rotary", r_k=1024, r_v=1024),
     "rotary wide values": dict(form="rotary", r_k=256, r_v=768),
+    "rotary rank 576": dict(form="rotary", r_k=576, r_v=576),
+    "rotary rank 768, 64 heads": dict(form="rotary", h_q=64, h_kv=8, r_k=768, r_v=736),
+    "rotary wide keys": dict(form="rotary", h_q=24, h_kv=12, r_k=800, r_v=96),
+    "rotary groups of 12": dict(form="rotary", h_q=60, h_kv=5, r_k=416, r_v=448),
+    "rotary group of 20": dict(form="rotary", h_q=40, h_kv=2, r_k=224, r_v=32),
+    "rotary d 64, rank 608": dict(form="rotary", h_q=20, h_kv=10, d=64, r_k=608, r_v=576),
 }
 
 
@@ -155,14 +161,14 @@ def test_lengths(name):
     Cache8(ctx=LENGTHS, **SHAPES[name]).check()
 
 
-@pytest.mark.parametrize("name", ["plain 8b", "plain groups of 20", "absorbed 8b", "absorbed 64 heads", "rotary 8b", "rotary 70b", "rotary uneven", "rotary rank 1024"])
+@pytest.mark.parametrize("name", ["plain 8b", "plain groups of 20", "absorbed 8b", "absorbed 64 heads", "rotary 8b", "rotary 70b", "rotary uneven", "rotary rank 1024", "rotary rank 768, 64 heads", "rotary groups of 12"])
 @pytest.mark.parametrize("ctx", [[3001], [1, 2500, 700, 1337]])
 def test_longer_contexts(name, ctx):
     Cache8(ctx=ctx, seed=11, **SHAPES[name]).check()
 
 
 FORMS = {"plain": dict(form="plain", h_q=8, h_kv=2), "absorbed": dict(form="absorbed", h_q=8, h_kv=2, r_k=160, r_v=128),
-         "rotary": dict(form="rotary", h_q=8, h_kv=2, r_k=192, r_v=256), "rotary any": dict(form="rotary", h_q=6, h_kv=3, d=64, r_k=64, r_v=96)}
+         "rotary": dict(form="rotary", h_q=8, h_kv=2, r_k=192, r_v=256), "rotary wide": dict(form="rotary", h_q=24, h_kv=2, r_k=160, r_v=192), "rotary any": dict(form="rotary", h_q=6, h_kv=3, d=64, r_k=64, r_v=96)}
 
 
 @pytest.mark.parametrize("name", FORMS)
