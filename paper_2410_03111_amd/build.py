@@ -20,6 +20,8 @@ HIP_FLAGS = [
     # packed-fp32 forms are switched off on the test machines
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 ]
+# results of matrix instructions in the half of the register file that vector instructions can use (the factor fills the other half)
+FILE_FLAGS = {"lorc_decode_q8_wide.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 NOISE = ("packed-fp32-ops", "is not a recognized feature")
 
 
@@ -46,7 +48,7 @@ def build(verbose: bool = False) -> str:
     for s in sources():
         o = os.path.join(OBJ, os.path.basename(s) + ".o")
         if s.endswith(".hip"):
-            jobs.append(([hipcc, *COMMON, *HIP_FLAGS, "-c", s, "-o", o], o))
+            jobs.append(([hipcc, *COMMON, *HIP_FLAGS, *FILE_FLAGS.get(os.path.basename(s), []), "-c", s, "-o", o], o))
         else:  # plain host C++: hipcc would treat it as device code
             jobs.append(([cxx, *COMMON, "-c", s, "-o", o], o))
     with ThreadPoolExecutor(max_workers=min(8, len(jobs))) as ex:

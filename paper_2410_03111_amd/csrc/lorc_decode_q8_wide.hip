@@ -139,35 +139,29 @@ __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeP
     const uint32_t ok = ~(uint32_t)(id >> 31);
     return dma_rsrc(reinterpret_cast<const unsigned char*>(p.cache) + (size_t)((uint32_t)id & ok) * page_bytes, page_bytes & ok);
   };
-  auto copy_scales = [&](const u32x4& r, int part, int buf, uint32_t lane4) {  // part: 0 K, 1 V
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      dma_256(r, uniform_u32(s_lds + (uint32_t)((2 * part + buf) * kWideScales + 256 * i)), lane4, uniform_u32((uint32_t)(64 * (r_k + r_v + (part ? gk : 0)) + 256 * i)));
+  const uint32_t lane4 = 4u * (uint32_t)lane, lane16 = 16u * (uint32_t)lane;
+  constexpr int NKC = (2 * NS + NW - 1) / NW, NVC = VB;  // copies per wave, and two of scale bytes each
+  auto copy_scales = [&](const u32x4& r, int part, int buf, int i) {  // part: 0 K, 1 V
+    dma_256(r, uniform_u32(s_lds + (uint32_t)((2 * part + buf) * kWideScales + 256 * i)), lane4, uniform_u32((uint32_t)(64 * (r_k + r_v + (part ? gk : 0)) + 256 * i)));
   };
-  auto copy_k = [&](int id, int t) {
-    const u32x4 r = rsrc_of(id);
+  auto copy_k = [&](const u32x4& r, int t, int i) {
     const int buf = t & 1, sb = t & 1;
-    const uint32_t lane4 = 4u * (uint32_t)lane, lane16 = 16u * (uint32_t)lane;
-#pragma unroll
-    for (int i = 0; i < (2 * NS + NW - 1) / NW; ++i) {
-      const int c = w + NW * i < k_rows ? w + NW * i : k_rows - 1;
-      dma_1k(r, uniform_u32(k_lds + (uint32_t)(buf * NS * 2048 + c * 1024)), lane16, uniform_u32((uint32_t)(sb * k_rows + c) * 1024u));
-    }
-    copy_scales(r, 0, buf, lane4);
+    if (i >= NKC) return copy_scales(r, 0, buf, i - NKC);
+    const int c = w + NW * i < k_rows ? w + NW * i : k_rows - 1;
+    dma_1k(r, uniform_u32(k_lds + (uint32_t)(buf * NS * 2048 + c * 1024)), lane16, uniform_u32((uint32_t)(sb * k_rows + c) * 1024u));
   };
-  auto copy_v = [&](int id, int t) {
-    const u32x4 r = rsrc_of(id);
+  auto copy_v = [&](const u32x4& r, int t, int i) {
     const int buf = t & 1, sb = t & 1;
-    const uint32_t lane4 = 4u * (uint32_t)lane, lane16 = 16u * (uint32_t)lane;
-#pragma unroll
-    for (int i = 0; i < VB; ++i) {
-      const int c = w + NW * i < v_rows ? w + NW * i : v_rows - 1;
-      dma_1k(r, uniform_u32(v_lds + (uint32_t)(buf * VB * 4096 + c * 1024)), lane16, uniform_u32((uint32_t)(64 * r_k + (c * 4 + 2 * sb) * 512)));
-    }
-    copy_scales(r, 1, buf, lane4);
+    if (i >= NVC) return copy_scales(r, 1, buf, i - NVC);
+    const int c = w + NW * i < v_rows ? w + NW * i : v_rows - 1;
+    dma_1k(r, uniform_u32(v_lds + (uint32_t)(buf * VB * 4096 + c * 1024)), lane16, uniform_u32((uint32_t)(64 * r_k + (c * 4 + 2 * sb) * 512)));
   };
   int id_cur = id_use(id_read(0), 0), id_next = id_use(id_read(1), 1);
-  copy_k(id_cur, 0);
+  {
+    const u32x4 r = rsrc_of(id_cur);
+#pragma unroll
+    for (int i = 0; i < NKC + 2; ++i) copy_k(r, 0, i);
+  }
 
   f32x4s o[2 * VB];
 #pragma unroll
@@ -176,6 +170,12 @@ __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeP
 #pragma unroll
   for (int j = 0; j < 16; ++j) acc[j] = prev_acc[j] = zero16[j] = 0.f;
   __builtin_amdgcn_s_waitcnt(0);  // the factor's loads too: none of them may be waited for inside the loop
+  // The factor lives in the accumulation half of the register file, which the products read as well; o does not, because it is rescaled by
+  // vector instructions on every half page (96 moves between the halves otherwise).
+#pragma unroll
+  for (int s = 0; s < NS; ++s)
+#pragma unroll
+    for (int u = 0; u < 2; ++u) asm volatile("" : "+a"(fac[s][u]));
 
   // ---- pieces of the stream
   const unsigned char* k_src = kbuf + lane * 8;
@@ -301,8 +301,7 @@ __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeP
     const int pos0 = begin + t * T, buf = t & 1, prev = buf ^ 1;
     dma_barrier<0>();  // this half page's K, the previous one's V; every wave is through the previous stream
     const int id_raw = id_read(t + 2);
-    copy_v(id_cur, t);
-    copy_k(id_next, t + 1);
+    const u32x4 r_next = rsrc_of(id_next), r_cur = rsrc_of(id_cur);
     f16x8 kf[2];
     f32x16 sa;
     Softmax sm;
@@ -319,6 +318,14 @@ __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeP
       __builtin_amdgcn_sched_barrier(0);
       acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fac[s][part], c[s % 2], x == 0 ? zero16 : acc, 0, 0, s & 3, fac_scale[s >> 2], (s >> 1) & 3,
                                                             k_scale[s >> 3]);
+      // -- the copies, spread over the first half of the stream: the next half page's K, this one's V
+      static_for<NKC + NVC + 4>([&](auto i_c) {
+        constexpr int i = decltype(i_c)::value;
+        if constexpr (x == at(i * 16 / (NKC + NVC + 4))) {
+          if constexpr (i < NKC + 2) copy_k(r_next, t + 1, i);
+          else copy_v(r_cur, t, i - NKC - 2);
+        }
+      });
       // -- the previous half page: rotation and scores
       static_for<4>([&](auto i_c) {
         if constexpr (x == at(decltype(i_c)::value)) rotate(kf, i_c);
