@@ -360,8 +360,8 @@ int lorc_quantize_latents(const lorc_layer_desc* desc, const void* cache, const 
  * lorc_decode_attention_absorbed on the values that the pages stand for, with cache and n_pages those of the 8-bit pool.
  *   workspace   lorc_decode_quantized_workspace_bytes (lorc_decode_plain_..., lorc_decode_absorbed_...) bytes, 256-byte aligned, or as many as any call
  *               with at least this b and max_ctx asks for
- * rotary: ranks up to 1024;  uncompressed: head_dim 128, rank_k = rank_v = n;  absorbed: ranks up to 1024;  64 query heads each;
- * otherwise the workspace size is 0 and the call LORC_EUNSUPPORTED. */
+ * rotary: ranks up to 1024, max_ctx up to 2^22;  uncompressed: head_dim 128, rank_k = rank_v = n, max_ctx up to 2^30;  absorbed: ranks up to 1024,
+ * max_ctx up to 2^25;  64 query heads each;  otherwise the workspace size is 0 and the call LORC_EUNSUPPORTED. */
 size_t lorc_decode_quantized_workspace_bytes(const lorc_layer_desc* desc, int32_t b, int32_t max_ctx);
 int lorc_decode_attention_quantized(const lorc_layer_desc* desc, const void* q, const int32_t* q_pos, const int32_t* ctx_len, int32_t b,
                              int32_t max_ctx, const void* packed, const void* cache_q8, const int32_t* block_table, int32_t max_pages,

@@ -151,7 +151,7 @@ extern "C" {
 
 size_t lorc_packed_bytes(const lorc_layer_desc* desc) {
   if (!desc || check_desc(*desc) != LORC_OK) return 0;
-  return packed_total_elems(desc->d_model, desc->rank_k, desc->rank_v, desc->n_kv_heads * desc->head_dim, desc->head_dim) * 2;
+  return packed_total_elems(desc->d_model, desc->rank_k, desc->rank_v, desc->n_kv_heads * desc->head_dim) * 2;
 }
 
 int lorc_pack_factors(const lorc_layer_desc* desc, const void* A_k, const void* A_v, const void* B_k,
@@ -531,7 +531,7 @@ int decode_q8(const lorc_layer_desc* desc, Q8Form form, const void* q, const int
   const bool rotary = form != Q8Form::kAbsorbed;
   if (int rc = decode_args(desc, q, q_pos, rotary, ctx_len, b, max_ctx, packed, cache, block_table, max_pages, n_pages, out, workspace))
     return rc;
-  if (!q8_shape_ok(*desc, form)) return LORC_EUNSUPPORTED;
+  if (!q8_shape_ok(*desc, form, max_ctx)) return LORC_EUNSUPPORTED;
   int n_cus = 0;
   if (int rc = device_ready(&n_cus)) return rc;
   const DecodePlan plan = make_q8_plan_within(*desc, form, b, max_ctx, n_cus, workspace_bytes);

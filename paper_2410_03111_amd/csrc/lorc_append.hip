@@ -53,8 +53,8 @@ __global__ void pack_factors_kernel(const uint16_t* __restrict__ A_k, const uint
 // B_k as pairs of e4m3 codes.  The first is the entry rounded to four significant bits, the second what that leaves: together the eight
 // bits of a bf16 entry, except below 2^-10 of the run's largest code unit, where what is lost is 5e-6 of the run's largest
 // entry at most.  One thread per column and run of 64 latent indices.
-__global__ __launch_bounds__(256) void pack_codes_kernel(const uint16_t* __restrict__ B_k, unsigned char* __restrict__ coded, int r_k, int n) {
-  const int steps = coded_steps(128, r_k);
+__global__ __launch_bounds__(256) void pack_codes_kernel(const uint16_t* __restrict__ B_k, unsigned char* __restrict__ coded, int r_k, int n, int head_dim) {
+  const int steps = coded_steps(r_k);
   const int i = blockIdx.x * 256 + threadIdx.x, c = i % n, s = i / n;
   if (s >= steps) return;
   float x[64];
@@ -68,7 +68,7 @@ __global__ __launch_bounds__(256) void pack_codes_kernel(const uint16_t* __restr
   }
   const int byte = scale_byte(most);
   const float inv = inverse_scale(byte);
-  uint32_t* dst = reinterpret_cast<uint32_t*>(coded) + (size_t)(coded_block(c) * steps + s) * 1024 + coded_row(c) * 4;
+  uint32_t* dst = reinterpret_cast<uint32_t*>(coded) + (size_t)(coded_block(head_dim, c) * steps + s) * 1024 + coded_row(head_dim, c) * 4;
 #pragma unroll
   for (int w = 0; w < 16; ++w) {  // word w: entries 4 w .. 4 w + 3 of the run
     int hi, lo;
@@ -77,7 +77,7 @@ __global__ __launch_bounds__(256) void pack_codes_kernel(const uint16_t* __restr
     dst[at] = (uint32_t)hi;
     dst[512 + at] = (uint32_t)lo;
   }
-  unsigned char* bytes = coded + (size_t)steps * n * 128 + (size_t)(coded_block(c) * 32 + coded_row(c)) * kCodedMaxSteps;
+  unsigned char* bytes = coded + (size_t)steps * n * 128 + (size_t)(coded_block(head_dim, c) * 32 + coded_row(head_dim, c)) * kCodedMaxSteps;
   bytes[s] = (unsigned char)byte;
   if (s == 0)  // runs past the rank multiply zeros: by anything but NaN (255)
     for (int u = steps; u < kCodedMaxSteps; ++u) bytes[u] = 127;
@@ -792,10 +792,10 @@ int launch_pack(const lorc_layer_desc& d, const void* A_k, const void* A_v, cons
                              (const uint16_t*)B_k, (const uint16_t*)B_v, (uint16_t*)packed, d.d_model, d.rank_k, d.rank_v, n,
                              d.head_dim, d.rope_base))
     return rc;
-  const int steps = coded_steps(d.head_dim, d.rank_k);
+  const int steps = coded_steps(d.rank_k);
   if (steps == 0 || B_k == nullptr) return LORC_OK;
   return launch_kernel(pack_codes_kernel, dim3((steps * n + 255) / 256), dim3(256), 0, s, (const uint16_t*)B_k,
-                       static_cast<unsigned char*>(packed) + packed_off_coded_bytes(d.d_model, d.rank_k, d.rank_v, n), d.rank_k, n);
+                       static_cast<unsigned char*>(packed) + packed_off_coded_bytes(d.d_model, d.rank_k, d.rank_v, n), d.rank_k, n, d.head_dim);
 }
 
 int set_kernel_attributes_append() {

@@ -18,28 +18,23 @@ constexpr float kNegInfQ = -__builtin_huge_valf();
 constexpr double kTurns = 0.15915494309189533576888;  // 1 / 2 pi
 }  // namespace
 
-// ------------------------------------------------------------------------------------------------ any shape
-// One workgroup of four waves per (sequence, context split, KV head), or block of 32 heads where the query is absorbed, 32
-// positions at a time.  The step's K codes are widened once into LDS (bf16, operand order); rotary: wave w rebuilds 16 coordinates of the
-// head and their partners, rotates them by the offset inside the step (the base goes to the queries) and scores its share of the
-// head; absorbed: wave w takes every fourth k-step.  Partial scores meet in LDS, eight lanes per head take the softmax, and wave w
-// owns every fourth block of 32 value latents, whose codes it loads itself.  Serves what the kernels below do not.
-template <int HD, bool ABSORBED>
+// ------------------------------------------------------------------------------------------------ absorbed query, ranks above 512
+// One workgroup of four waves per (sequence, context split, block of 32 query heads), 32 positions at a time.  The step's K codes are
+// widened once into LDS (bf16, operand order), wave w takes every fourth k-step of the scores, partial scores meet in LDS, eight lanes
+// per head take the softmax, and wave w owns every fourth block of 32 value latents, whose codes it loads itself, ahead of the scores.
 __global__ __launch_bounds__(256, 1) void decode_q8_kernel(DecodeParams p) {
-  constexpr int HALF = HD / 2, T = 32, NBW = 8;
+  constexpr int T = 32, NBW = 8;
   extern __shared__ __align__(16) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5, l32 = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r_k = p.r_k, r_v = p.r_v, nks = r_k >> 4, gk = q8_groups(r_k), gv = q8_groups(r_v), nb = r_v >> 5;
-  const int n_units = ABSORBED ? (p.h_q + 31) / 32 : p.h_kv;
+  const int n_units = (p.h_q + 31) / 32;
   const int unit = blockIdx.x % n_units, ss = blockIdx.x / n_units, split = ss % p.n_splits, seq = ss / p.n_splits;
-  const int h0 = ABSORBED ? 32 * unit : unit * p.G;
-  const int nh = ABSORBED ? (p.h_q - h0 < 32 ? p.h_q - h0 : 32) : p.G;
+  const int h0 = 32 * unit, nh = p.h_q - h0 < 32 ? p.h_q - h0 : 32;
   uint16_t* kt = reinterpret_cast<uint16_t*>(smem);                       // [nks][64 lanes][8]
   float* sp = reinterpret_cast<float*>(smem + (size_t)r_k * 64);          // [4 waves][32 heads][32 positions]
   uint16_t* pb = reinterpret_cast<uint16_t*>(sp + 4 * 32 * T);            // [gv][2][64 lanes][8]
-  uint32_t* qr = reinterpret_cast<uint32_t*>(pb + (size_t)gv * 1024);     // [32 heads][HALF] fp16 pairs (rotary)
-  float* al = reinterpret_cast<float*>(qr + 32 * HALF);                   // [32]
+  float* al = reinterpret_cast<float*>(pb + (size_t)gv * 1024);           // [32]
   float* l_fin = al + 32;
 
   int ctx = p.ctx_len[seq];
@@ -57,8 +52,6 @@ __global__ __launch_bounds__(256, 1) void decode_q8_kernel(DecodeParams p) {
   for (int i = 0; i < NBW; ++i) o[i] = zero16;
   const int sh = tid >> 3, s8 = tid & 7;  // softmax: head, and which four of the positions
   float m_run = kNoWeight, l_run = 0.f;
-  const int wq = w;
-  const bool rebuilds = ABSORBED || w < HD / 32;
 
   for (int pos0 = t_begin; pos0 < t_end; pos0 += T) {
     const int id = __builtin_amdgcn_readfirstlane(p.block_table[(size_t)seq * p.max_pages + pos0 / kPage]), sb = (pos0 / T) & 1;
@@ -73,64 +66,38 @@ __global__ __launch_bounds__(256, 1) void decode_q8_kernel(DecodeParams p) {
       dst[0] = codes_bf16(u32x2{v[0], v[1]}, pow2_of(sc & 255u));
       dst[1] = codes_bf16(u32x2{v[2], v[3]}, pow2_of((sc >> 8) & 255u));
     }
-    if constexpr (!ABSORBED) {  // queries rotated by the distance to the step's first position
-      const int i = tid % HALF;
-      const double turns = (double)(p.q_pos[seq] - pos0) * p.rope_tab[i] * kTurns;
-      const float fr = (float)(turns - rint(turns)), cs = __builtin_amdgcn_cosf(fr), sn = __builtin_amdgcn_sinf(fr);
-      for (int h = tid / HALF; h < nh; h += 256 / HALF) {
-        const uint16_t* src = p.q + ((size_t)seq * p.h_q + h0 + h) * HD + i;
-        const float x = bf16_to_float(src[0]) * p.q_scale, y = bf16_to_float(src[HALF]) * p.q_scale;
-        half2_t v;
-        v[0] = static_cast<_Float16>(x * cs - y * sn);
-        v[1] = static_cast<_Float16>(y * cs + x * sn);
-        qr[h * HALF + i] = __builtin_bit_cast(uint32_t, v);
+    // ---- what the later phases need of the page travels meanwhile
+    uint32_t ub[8];  // value scale bytes of the thread's four positions, per group
+#pragma unroll
+    for (int g = 0; g < 8; ++g)
+      ub[g] = g < gv ? (ok ? __builtin_amdgcn_raw_buffer_load_b32(page, (gk + g) * kPage + 32 * sb + 4 * s8, codes, 0) : 0x7f7f7f7fu) : 0u;
+    u32x2 vraw[NBW][2];
+#pragma unroll
+    for (int i = 0; i < NBW; ++i)
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        const int jb = w + 4 * i < nb ? w + 4 * i : 0;
+        vraw[i][ks] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(page, lane * 8, kPage * r_k + (jb * 4 + 2 * sb + ks) * 512, 0));
       }
-    }
     __syncthreads();
     // ---- scores
-    if (rebuilds) {
+    {
       const uint16_t* kl = kt + (size_t)lane * 8;
+      const uint16_t* qsrc = p.q + ((size_t)seq * p.h_q + h0 + (l32 < nh ? l32 : 0)) * r_k + 8 * hf;
       f32x16 sa = zero16;
-      if constexpr (ABSORBED) {
-        const uint16_t* qsrc = p.q + ((size_t)seq * p.h_q + h0 + (l32 < nh ? l32 : 0)) * r_k + 8 * hf;
-        for (int ks = w; ks < nks; ks += 4) sa = mfma32(load_frag(qsrc + 16 * ks), load_frag(kl + (size_t)ks * 512), sa);
+#pragma unroll 4
+      for (int ks = w; ks < nks; ks += 4) sa = mfma32(load_frag(qsrc + 16 * ks), load_frag(kl + (size_t)ks * 512), sa);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) sa[j] *= p.q_scale;
-      } else {
-        // rows 0 .. 15 of the rebuilt block are the coordinates 16 w + row, rows 16 .. 31 their partners
-        const int col = unit * HD + 16 * wq + l32 + (l32 < 16 ? 0 : HALF - 16);
-        f32x16 acc = zero16;
-        for (int ks = 0; ks < nks; ++ks) acc = mfma32(load_frag(p.bk + b_tile_index(r_k, 16 * ks + 8 * hf, col)), load_frag(kl + (size_t)ks * 512), acc);
-        f16x8 kf[2];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float2 cs = p.lane_cs[l32 * HALF + 16 * wq + acc_row(j, hf)];
-          const float x = acc[j], y = acc[j + 8];
-          kf[j >> 2][2 * (j & 3)] = static_cast<_Float16>(x * cs.x - y * cs.y);
-          kf[j >> 2][2 * (j & 3) + 1] = static_cast<_Float16>(y * cs.x + x * cs.y);
-        }
-        const uint32_t* qs = qr + (l32 < nh ? l32 : 0) * HALF + 16 * wq + 4 * hf;
-        sa = mfma32_f16(__builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4*>(qs)), kf[0], sa);
-        sa = mfma32_f16(__builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4*>(qs + 8)), kf[1], sa);
-      }
-#pragma unroll
-      for (int j = 0; j < 16; ++j) sp[(w * 32 + acc_row(j, hf)) * T + l32] = sa[j];
+      for (int j = 0; j < 16; ++j) sp[(w * 32 + acc_row(j, hf)) * T + l32] = sa[j] * p.q_scale;
     }
     __syncthreads();
     // ---- softmax: eight lanes per head, four positions each
     {
-      const int n_part = ABSORBED ? 4 : HD / 32;
-      float s[4], kmax[4];
-      uint32_t ub[8];  // scale bytes of the four positions, per group
-      float mx = kNegInfQ;
-#pragma unroll
-      for (int g = 0; g < 8; ++g)
-        ub[g] = g < gv ? (ok ? __builtin_amdgcn_raw_buffer_load_b32(page, (gk + g) * kPage + 32 * sb + 4 * s8, codes, 0) : 0x7f7f7f7fu) : 0u;
+      float s[4], mx = kNegInfQ;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int pos = 4 * s8 + e;
-        s[e] = 0.f;
-        for (int u = 0; u < n_part; ++u) s[e] += sp[(u * 32 + sh) * T + pos];
+        s[e] = (sp[sh * T + pos] + sp[(32 + sh) * T + pos]) + (sp[(64 + sh) * T + pos] + sp[(96 + sh) * T + pos]);
         if (pos0 + pos >= t_end) s[e] = kNegInfQ;
         uint32_t top = 127 + kLeastExp;
 #pragma unroll
@@ -138,8 +105,7 @@ __global__ __launch_bounds__(256, 1) void decode_q8_kernel(DecodeParams p) {
           const uint32_t b = (ub[g] >> (8 * e)) & 255u;
           top = g < gv && b > top ? b : top;
         }
-        kmax[e] = (float)top - 127.f;
-        mx = fmaxf(mx, s[e] + kmax[e]);
+        mx = fmaxf(mx, s[e] + ((float)top - 127.f));
       }
 #pragma unroll
       for (int step = 1; step < 8; step <<= 1) mx = fmaxf(mx, __shfl_xor(mx, step, 64));
@@ -150,16 +116,13 @@ __global__ __launch_bounds__(256, 1) void decode_q8_kernel(DecodeParams p) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int pos = 4 * s8 + e;
-        const bool in = pos0 + pos < t_end;
-        l_run += in ? exp2f(s[e] - m_new) : 0.f;
+        const float pe = pos0 + pos < t_end ? exp2f(s[e] - m_new) : 0.f;
+        l_run += pe;
 #pragma unroll
-        for (int g = 0; g < 8; ++g) {
-          if (g < gv) {
-            const float k = (float)((ub[g] >> (8 * e)) & 255u) - 127.f;
-            const float pe = in ? exp2f(s[e] + k - m_new) : 0.f;
-            pb[((size_t)(g * 2 + (pos >> 4)) * 64 + sh + 32 * ((pos & 15) >> 3)) * 8 + (pos & 7)] = f16_bits(pe);
-          }
-        }
+        for (int g = 0; g < 8; ++g)
+          if (g < gv)
+            pb[((size_t)(g * 2 + (pos >> 4)) * 64 + sh + 32 * ((pos & 15) >> 3)) * 8 + (pos & 7)] =
+                f16_bits(__builtin_amdgcn_ldexpf(pe, (int)((ub[g] >> (8 * e)) & 255u) - 127));
       }
     }
     __syncthreads();
@@ -174,7 +137,7 @@ __global__ __launch_bounds__(256, 1) void decode_q8_kernel(DecodeParams p) {
           for (int j = 0; j < 16; ++j) o[i][j] *= al[acc_row(j, hf)];
 #pragma unroll
           for (int ks = 0; ks < 2; ++ks) {
-            u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(page, lane * 8, kPage * r_k + (jb * 4 + 2 * sb + ks) * 512, 0));
+            u32x2 v = vraw[i][ks];
             if (left < T) v = keep_bytes(v, left - 16 * ks - 8 * hf);  // slots past the context hold anything, NaN codes too
             const f16x8 pf = load_frag_f16(pb + ((size_t)((jb >> 2) * 2 + ks) * 64 + lane) * 8);
             o[i] = mfma32_f16(pf, codes_f16(v), o[i]);
@@ -398,41 +361,43 @@ __global__ __launch_bounds__(256, 2) void decode_plain_q8_kernel(DecodeParams p)
 namespace {
 size_t align256q(size_t x) { return (x + 255) & ~(size_t)255; }
 size_t q8_lds_bytes(const lorc_layer_desc& d) {
-  return (size_t)d.rank_k * 64 + 4 * 32 * 32 * 4 + (size_t)q8_groups(d.rank_v) * 2048 + 32 * 64 * 4 + 2 * 32 * 4;
+  return (size_t)d.rank_k * 64 + 4 * 32 * 32 * 4 + (size_t)q8_groups(d.rank_v) * 2048 + 2 * 32 * 4;
 }
 }  // namespace
 
-bool q8_shape_ok(const lorc_layer_desc& d, Q8Form form) {
-  if (form == Q8Form::kPlain) return plain_shape_ok(d);
-  return d.rank_k <= kStreamMaxRank && d.rank_v <= kStreamMaxRank;
+namespace {
+// Which kernel, and how it divides a sequence: workgroups per (sequence, split), those that share a compute unit, the pages that a split
+// walks at most (their ids live in LDS).
+struct Q8Walk {
+  long units, per_cu, most;
+  int kernel;  // rotary: 1 stationary, 2 wide; absorbed: 1 ranks to 512, 0 above
+};
+Q8Walk q8_walk(const lorc_layer_desc& d, Q8Form form) {
+  constexpr long kAny = (1 << 30) / kPage;
+  if (form == Q8Form::kPlain) return {(d.n_kv_heads * ((d.n_q_heads / d.n_kv_heads + 15) / 16) + 3) / 4, 2, kAny, 0};
+  if (form == Q8Form::kAbsorbed) {
+    const bool fast = q8_absorbed_shape_ok(d);
+    return {(d.n_q_heads + 31) / 32, 1, fast ? q8_absorbed_max_tiles() : kAny, fast};
+  }
+  if (q8_stationary_shape_ok(d)) return {(d.n_kv_heads + 1) / 2, 1, q8_stationary_max_tiles(), 1};
+  return {q8_wide_units(d), 1, q8_wide_max_tiles(), 2};
+}
+}  // namespace
+
+bool q8_shape_ok(const lorc_layer_desc& d, Q8Form form, int max_ctx) {
+  if (form == Q8Form::kPlain ? !plain_shape_ok(d) : d.rank_k > kStreamMaxRank || d.rank_v > kStreamMaxRank) return false;
+  // the merge joins 512 splits; and a split's end has to stay below 2^31
+  return max_ctx <= (1 << 30) && (max_ctx + kPage - 1) / kPage <= 512 * q8_walk(d, form).most;
 }
 
 DecodePlan make_q8_plan(const lorc_layer_desc& d, Q8Form form, int b, int max_ctx, int n_cus, int max_splits) {
   DecodePlan pl{};
-  if (!q8_shape_ok(d, form)) return pl;
+  if (!q8_shape_ok(d, form, max_ctx)) return pl;
   pl.tile = kPage;
   int n_tiles = (max_ctx + kPage - 1) / kPage;
   if (n_tiles < 1) n_tiles = 1;
-  // units: workgroups per (sequence, split); per_cu: those that share a compute unit; most: pages that a split walks at most
-  long units, per_cu = 1, most = n_tiles;
-  if (form == Q8Form::kPlain) {
-    units = (d.n_kv_heads * ((d.n_q_heads / d.n_kv_heads + 15) / 16) + 3) / 4;
-    per_cu = 2;
-  } else if (form == Q8Form::kAbsorbed) {
-    units = (d.n_q_heads + 31) / 32;
-    pl.stationary = q8_absorbed_shape_ok(d);
-    if (pl.stationary) most = q8_absorbed_max_tiles();
-  } else if (q8_stationary_shape_ok(d)) {
-    units = (d.n_kv_heads + 1) / 2;
-    pl.stationary = 1;
-    most = q8_stationary_max_tiles();
-  } else if (q8_wide_shape_ok(d)) {
-    units = d.n_kv_heads * ((d.n_q_heads / d.n_kv_heads + 15) / 16);
-    pl.stationary = 2;
-    most = q8_wide_max_tiles();
-  } else {
-    units = d.n_kv_heads;
-  }
+  const auto [units, per_cu, most, kernel] = q8_walk(d, form);
+  pl.stationary = kernel;
   const long least = (n_tiles + most - 1) / most;
   long ns = (per_cu * (n_cus > 0 ? n_cus : 256) + b * units - 1) / (b * units);
   if (ns > 64) ns = 64;
@@ -464,9 +429,8 @@ DecodePlan make_q8_plan_within(const lorc_layer_desc& d, Q8Form form, int b, int
 }
 
 int set_kernel_attributes_decode_q8() {
-  for (void (*k)(DecodeParams) : {decode_q8_kernel<64, false>, decode_q8_kernel<128, false>, decode_q8_kernel<64, true>, decode_q8_kernel<128, true>})
-    if (hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess) return LORC_EHIP;
-  return LORC_OK;
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(decode_q8_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) == hipSuccess
+             ? LORC_OK : LORC_EHIP;
 }
 
 int launch_decode_q8(const lorc_layer_desc& d, Q8Form form, const DecodeParams& p, const DecodePlan& plan, hipStream_t s) {
@@ -480,19 +444,14 @@ int launch_decode_q8(const lorc_layer_desc& d, Q8Form form, const DecodeParams& 
   }
   if (plan.stationary) {
     if (int rc = form == Q8Form::kAbsorbed ? launch_decode_q8_absorbed(p, s)
-                 : plan.stationary == 2    ? launch_decode_q8_wide(p, s)
+                 : plan.stationary == 2    ? launch_decode_q8_wide(d, p, s)
                                            : launch_decode_q8_stationary(p, s))
       return rc;
     return launch_decode_merge(p, false, s);
   }
   const size_t lds = q8_lds_bytes(d);
   if (lds > 160 * 1024) return LORC_EUNSUPPORTED;
-  const bool absorbed = form == Q8Form::kAbsorbed;
-  const dim3 grid(units * (absorbed ? (p.h_q + 31) / 32 : p.h_kv));
-  if (int rc = launch_kernel(p.head_dim == 128 ? (absorbed ? decode_q8_kernel<128, true> : decode_q8_kernel<128, false>)
-                                               : (absorbed ? decode_q8_kernel<64, true> : decode_q8_kernel<64, false>),
-                             grid, dim3(256), lds, s, p))
-    return rc;
+  if (int rc = launch_kernel(decode_q8_kernel, dim3(units * ((p.h_q + 31) / 32)), dim3(256), lds, s, p)) return rc;
   return launch_decode_merge(p, false, s);
 }
 

@@ -96,7 +96,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
   i32x8 fac[NS][2];  // the factor: see the head of this file
   int fac_scale[2];
   {
-    const int n = p.h_kv * HD, steps = coded_steps(HD, r_k), block = (2 * hp + kvh) * 4 + wq;
+    const int n = p.h_kv * HD, steps = coded_steps(r_k), block = (2 * hp + kvh) * 4 + wq;
     const __amdgpu_buffer_rsrc_t r = make_rsrc(p.coded, (uint32_t)(steps * 128 + kCodedMaxSteps) * (uint32_t)n);
     const bool real = 2 * hp + kvh < p.h_kv;  // (the last pair of an odd number of heads)
 #pragma unroll
@@ -489,7 +489,7 @@ Q8StatKernel q8_stat_kernel(int ns) {
     default: return decode_q8_stationary_kernel<8, PPH>;
   }
 }
-int q8_stat_ns(int r_k) { return r_k <= 128 ? 2 : coded_steps(128, r_k); }
+int q8_stat_ns(int r_k) { return r_k <= 128 ? 2 : coded_steps(r_k); }
 }  // namespace
 
 bool q8_stationary_shape_ok(const lorc_layer_desc& d) {

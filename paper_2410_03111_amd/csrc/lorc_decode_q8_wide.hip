@@ -1,9 +1,9 @@
-// Rotary decode attention over 8-bit pages for what lorc_decode_q8_stat.hip has no room for: ranks from 544 to 1024, and groups of 9 to 32
-// query heads; head_dim 128.
+// Rotary decode attention over 8-bit pages for what lorc_decode_q8_stat.hip has no room for: ranks from 544 to 1024, groups of 9 to 32
+// query heads, head_dim 64.
 //
 // The same products (the pages' codes against B_k as pairs of e4m3 codes, held in registers), with one wave per SIMD: four waves of up
-// to 512 registers own one KV head of one (sequence, context split) and up to sixteen of its query heads; a wave holds 32 columns, 16
-// registers per 64 latent indices (256 at rank 1024).  Half pages of 32 positions keep K and V in two buffers each within the LDS.  A
+// to 512 registers own one KV head of head_dim 128 (or two of 64) of one (sequence, context split) and up to sixteen query heads; a wave
+// holds 32 columns, 16 registers per 64 latent indices (256 at rank 1024).  Half pages of 32 positions keep K and V in two buffers each within the LDS.  A
 // product takes 64 cycles of the matrix core and the next one of the wave waits for it, so everything else is laid between the
 // products of the next half page's rebuild: rotation and scores;  barrier;  softmax, queries;  barrier;  P' codes_V.
 #include "lorc_device.h"
@@ -29,20 +29,24 @@ __host__ __device__ constexpr size_t q8_wide_lds_bytes(int ns, int vb, int heads
 }  // namespace
 
 // NS: k-steps of 64 latent indices of K; VB: blocks of 32 value latents per wave; PPH: pairs of heads whose softmax a wave takes.
-template <int NS, int VB, int PPH>
+template <int HD, int NS, int VB, int PPH>
 __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeParams p) {
-  constexpr int HD = 128, HALF = 64, T = 32, NW = kWideWaves, NT = kWideThreads, HW = 8 * PPH, X = 2 * NS;
+  constexpr int HALF = HD / 2, T = 32, NW = kWideWaves, NT = kWideThreads, HW = 8 * PPH, X = 2 * NS;
+  constexpr int QW = HD / 32, KVW = NW / QW, HP = 16 / KVW;  // waves of a KV head, KV heads of a workgroup, query heads of each at most
   extern __shared__ __align__(16) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5, l32 = lane & 31, n16 = lane & 15, kg = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // workgroup -> (sequence, split, KV head, sixteen of its query heads); those of one (sequence, split) sit on one XCD
-  const int parts = (p.G + 15) >> 4, NQ = p.h_kv * parts;
+  // workgroup -> (sequence, split, KV heads, HP query heads of each); those of one (sequence, split) sit on one XCD
+  const int parts = (p.G + HP - 1) / HP, NQ = (p.h_kv + KVW - 1) / KVW * parts;
   const int grp = blockIdx.x / (8 * NQ), rem = blockIdx.x % (8 * NQ);
   const int hp = rem >> 3, unit_id = grp * 8 + (rem & 7);
   if (unit_id >= p.b * p.n_splits) return;
-  const int seq = unit_id / p.n_splits, split = unit_id % p.n_splits, g_kv = hp / parts;
+  const int seq = unit_id / p.n_splits, split = unit_id % p.n_splits, g_kv = hp / parts * KVW;
   const int r_k = p.r_k, r_v = p.r_v, gk = q8_groups(r_k), gv = q8_groups(r_v);
-  const int h0 = g_kv * p.G + 16 * (hp % parts), left = p.G - 16 * (hp % parts), n_heads = left < 16 ? left : 16;
+  const int part0 = HP * (hp % parts), left = p.G - part0, gp = left < HP ? left : HP;  // query heads of a KV head here
+  const int n_heads = (p.h_kv - g_kv < KVW ? p.h_kv - g_kv : KVW) * gp;
+  auto head_of = [&](int h) { return KVW == 1 ? g_kv * p.G + part0 + h : (g_kv + h / gp) * p.G + part0 + h % gp; };
+  const int kvh = w / QW, wq = w % QW;
 
   unsigned char* kbuf = smem;
   unsigned char* vbuf = kbuf + (size_t)2 * NS * 2048;
@@ -54,7 +58,7 @@ __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeP
   float* m_fin = alpha + 16;
   float* l_fin = m_fin + 16;
   double* turns_tab = reinterpret_cast<double*>(l_fin + 16);
-  int* ids = reinterpret_cast<int*>(turns_tab + HALF);
+  int* ids = reinterpret_cast<int*>(turns_tab + 64);
   const uint32_t k_lds = (uint32_t)(uintptr_t)kbuf, v_lds = (uint32_t)(uintptr_t)vbuf, s_lds = (uint32_t)(uintptr_t)sbytes;
 
   // ---- set-up
@@ -79,33 +83,35 @@ __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeP
 #pragma unroll
   for (int u = 0; u < 2 * PPH; ++u) {
     q_head[u] = w + 4 * u < n_heads ? w + 4 * u : n_heads - 1;
-    const uint16_t* src = p.q + ((size_t)seq * p.h_q + h0 + q_head[u]) * HD + lane;
+    const uint16_t* src = p.q + ((size_t)seq * p.h_q + head_of(q_head[u])) * HD + lane % HALF;
     q_raw[u] = (uint32_t)src[0] | (uint32_t)src[HALF] << 16;
   }
-  const double theta_lane = p.rope_tab[lane] * kInvTwoPi;
+  const double theta_lane = p.rope_tab[lane % HALF] * kInvTwoPi;
   half2_t rot[8];  // (cos, sin) of the position's offset in the half page, the lane's eight frequencies
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const float2 cs = p.lane_cs[l32 * HALF + 16 * w + acc_row(j, hf)];
+    const float2 cs = p.lane_cs[l32 * HALF + 16 * wq + acc_row(j, hf)];
     rot[j][0] = static_cast<_Float16>(cs.x);
     rot[j][1] = static_cast<_Float16>(cs.y);
   }
   i32x8 fac[NS][2];
   int fac_scale[4];
   {
-    const int n = p.h_kv * HD, steps = coded_steps(HD, r_k), block = g_kv * 4 + w;
+    const int n = p.h_kv * HD, steps = coded_steps(r_k), block = (g_kv + kvh) * QW + wq;
+    const bool real = g_kv + kvh < p.h_kv;  // (the last pair of an odd number of heads)
     const __amdgpu_buffer_rsrc_t r = make_rsrc(p.coded, (uint32_t)(steps * 128 + kCodedMaxSteps) * (uint32_t)n);
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         // (past the end: zeros; in the lane offset, which is what the bound is compared with)
-        const uint32_t at = s < steps ? (uint32_t)((block * steps + s) * 2 + u) * 2048u + lane * 16u : 0x7fff0000u;
+        const uint32_t at = real && s < steps ? (uint32_t)((block * steps + s) * 2 + u) * 2048u + lane * 16u : 0x7fff0000u;
         const u32x4 a = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0));
         const u32x4 b = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at + 1024u, 0, 0));
         fac[s][u] = i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
       }
-    const u32x4 sc = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (uint32_t)steps * n * 128u + (uint32_t)(block * 32 + l32) * (uint32_t)kCodedMaxSteps, 0, 0));
+    const u32x4 sc = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+        r, real ? (uint32_t)steps * n * 128u + (uint32_t)(block * 32 + l32) * (uint32_t)kCodedMaxSteps : 0x7fff0000u, 0, 0));
 #pragma unroll
     for (int c = 0; c < 4; ++c) fac_scale[c] = (int)sc[c];
   }
@@ -125,7 +131,7 @@ __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeP
       alpha[tid] = 1.f;
       l_fin[tid] = 0.f;
     }
-    if (tid < HALF) turns_tab[tid] = theta_lane;
+    if (tid < 64) turns_tab[tid] = theta_lane;
     if (tid < kWideTiles / 2) ids[tid] = my_id >= 0 && my_id < p.n_pages ? my_id : -1;
   }
   lds_barrier();
@@ -202,7 +208,7 @@ __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeP
       kf[j >> 2][2 * (j & 3) + 1] = static_cast<_Float16>(y * c + x * s);
     }
   };
-  const uint32_t* q_src = qrot + (size_t)(l32 < n_heads ? l32 : 0) * kStatQPitch + 16 * w + 4 * hf;
+  const uint32_t* q_src = qrot + (size_t)(kvh * gp + (l32 < gp && kvh * gp + l32 < n_heads ? l32 : 0)) * kStatQPitch + 16 * wq + 4 * hf;
   float* s_dst = sp + (size_t)(w * 16 + 4 * hf) * T + l32;
   auto score = [&](f32x16& sa, const f16x8 (&kf)[2], auto part_c) {
     constexpr int part = decltype(part_c)::value;
@@ -212,20 +218,24 @@ __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeP
 #pragma unroll
     for (int j = 0; j < 4 * PPH; ++j) s_dst[(8 * (j >> 2) + (j & 3)) * T] = sa[j];
   };
+  int sm_src[PPH];  // first partial score of the head at the lane's position
+#pragma unroll
+  for (int u = 0; u < PPH; ++u)
+    sm_src[u] = ((KVW == 1 ? 0 : sm_h[u] / gp) * QW * 16 + (KVW == 1 ? sm_h[u] : sm_h[u] % gp)) * T + l32;
   struct Softmax {
-    float a[4], s, mx, e;
+    float a[QW], s, mx, e;
     uint32_t ub[8];
   };
   auto softmax_load = [&](Softmax& sm, int u, int t) {
-    const float* src = sp + (size_t)sm_h[u] * T + l32;
+    const float* src = sp + sm_src[u];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) sm.a[q] = src[q * 16 * T];
+    for (int q = 0; q < QW; ++q) sm.a[q] = src[q * 16 * T];
     const unsigned char* at = sbytes + (2 + (t & 1)) * kWideScales + 32 * (t & 1) + l32;
 #pragma unroll
     for (int g = 0; g < 8; ++g) sm.ub[g] = at[g < gv ? 64 * g : 0];
   };
   auto softmax_max = [&](Softmax& sm, int valid) {
-    sm.s = l32 < valid ? (sm.a[0] + sm.a[1]) + (sm.a[2] + sm.a[3]) : kNegInfS;
+    sm.s = l32 < valid ? (QW == 4 ? (sm.a[0] + sm.a[1]) + (sm.a[2] + sm.a[3]) : sm.a[0] + sm.a[1]) : kNegInfS;
     uint32_t top = 127 + kLeastExp;
 #pragma unroll
     for (int g = 0; g < 8; ++g) top = top > sm.ub[g] ? top : sm.ub[g];
@@ -267,7 +277,7 @@ __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeP
       half2_t v;
       v[0] = static_cast<_Float16>(x * qr.cs - y * qr.sn);
       v[1] = static_cast<_Float16>(y * qr.cs + x * qr.sn);
-      qrot[(size_t)q_head[u] * kStatQPitch + lane] = __builtin_bit_cast(uint32_t, v);
+      qrot[(size_t)q_head[u] * kStatQPitch + lane % HALF] = __builtin_bit_cast(uint32_t, v);
     }
   };
   // O += P' codes: wave w owns blocks w, w + 4, ... of 32 value latents; accumulator 2 i + b: latents 32 (w + 4 i) + 2 n16 + b
@@ -406,10 +416,10 @@ __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeP
     l_fin[sm_h[u]] = rows.x + rows.y;
   }
   __syncthreads();
-  const size_t row0 = ((size_t)seq * p.n_splits + split) * p.h_q + h0;
+  const size_t row0 = ((size_t)seq * p.n_splits + split) * p.h_q;
   if (tid < n_heads) {
-    p.part_ml[(row0 + tid) * 2] = nt > 0 ? m_fin[tid] : kNegInfS;
-    p.part_ml[(row0 + tid) * 2 + 1] = l_fin[tid];
+    p.part_ml[(row0 + head_of(tid)) * 2] = nt > 0 ? m_fin[tid] : kNegInfS;
+    p.part_ml[(row0 + head_of(tid)) * 2 + 1] = l_fin[tid];
   }
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -419,7 +429,7 @@ __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeP
 #pragma unroll
       for (int i = 0; i < VB; ++i)
         if (w + NW * i < v_rows)
-          *reinterpret_cast<uint32_t*>(p.part_o + (row0 + h) * r_v + 32 * (w + NW * i) + 2 * n16) =
+          *reinterpret_cast<uint32_t*>(p.part_o + (row0 + head_of(h)) * r_v + 32 * (w + NW * i) + 2 * n16) =
               (uint32_t)f16_bits(o[2 * i][j] * inv) | ((uint32_t)f16_bits(o[2 * i + 1][j] * inv) << 16);
     }
   }
@@ -431,38 +441,49 @@ using Q8WideKernel = void (*)(DecodeParams);
 // latents that a kernel is padded to (the larger of K's and V's)
 int q8_wide_class(int r_k, int r_v) {
   const int r = r_k > r_v ? r_k : r_v;
-  return r <= 256 ? 256 : r <= 512 ? 512 : r <= 640 ? 640 : r <= 768 ? 768 : 1024;
+  return r <= 128 ? 128 : r <= 256 ? 256 : r <= 512 ? 512 : r <= 640 ? 640 : r <= 768 ? 768 : 1024;
 }
-template <int PPH>
+template <int HD, int PPH>
 Q8WideKernel q8_wide_kernel(int cls) {
   switch (cls) {
-    case 256: return decode_q8_wide_kernel<4, 2, PPH>;
-    case 512: return decode_q8_wide_kernel<8, 4, PPH>;
-    case 640: return decode_q8_wide_kernel<10, 5, PPH>;
-    case 768: return decode_q8_wide_kernel<12, 6, PPH>;
-    default: return decode_q8_wide_kernel<16, 8, PPH>;
+    case 128: return decode_q8_wide_kernel<HD, 2, 1, PPH>;
+    case 256: return decode_q8_wide_kernel<HD, 4, 2, PPH>;
+    case 512: return decode_q8_wide_kernel<HD, 8, 4, PPH>;
+    case 640: return decode_q8_wide_kernel<HD, 10, 5, PPH>;
+    case 768: return decode_q8_wide_kernel<HD, 12, 6, PPH>;
+    default: return decode_q8_wide_kernel<HD, 16, 8, PPH>;
   }
+}
+Q8WideKernel q8_wide_kernel(int head_dim, int cls, bool one) {
+  if (head_dim == 128) return one ? q8_wide_kernel<128, 1>(cls) : q8_wide_kernel<128, 2>(cls);
+  return one ? q8_wide_kernel<64, 1>(cls) : q8_wide_kernel<64, 2>(cls);
 }
 }  // namespace
 
-bool q8_wide_shape_ok(const lorc_layer_desc& d) { return d.head_dim == 128 && d.rank_k <= kCodedMaxRank && d.rank_v <= 1024; }
+// Workgroups of a (sequence, split): one KV head of 128 coordinates and sixteen of its query heads, or two of 64 and eight of each.
+int q8_wide_units(const lorc_layer_desc& d) {
+  const int G = d.n_q_heads / d.n_kv_heads;
+  return d.head_dim == 128 ? d.n_kv_heads * ((G + 15) / 16) : (d.n_kv_heads + 1) / 2 * ((G + 7) / 8);
+}
 
 int q8_wide_max_tiles() { return kWideTiles / 2; }
 
 int set_kernel_attributes_decode_q8_wide() {
-  for (int cls : {256, 512, 640, 768, 1024})
-    for (Q8WideKernel k : {q8_wide_kernel<1>(cls), q8_wide_kernel<2>(cls)})
-      if (hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess)
-        return LORC_EHIP;
+  for (int head_dim : {64, 128})
+    for (int cls : {128, 256, 512, 640, 768, 1024})
+      for (bool one : {false, true})
+        if (hipFuncSetAttribute(reinterpret_cast<const void*>(q8_wide_kernel(head_dim, cls, one)), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                160 * 1024) != hipSuccess)
+          return LORC_EHIP;
   return LORC_OK;
 }
 
-int launch_decode_q8_wide(const DecodeParams& p, hipStream_t s) {
-  const int cls = q8_wide_class(p.r_k, p.r_v), nq = p.h_kv * ((p.G + 15) / 16), units = p.b * p.n_splits;
-  const bool one = p.G <= 8;
+int launch_decode_q8_wide(const lorc_layer_desc& d, const DecodeParams& p, hipStream_t s) {
+  const int cls = q8_wide_class(p.r_k, p.r_v), nq = q8_wide_units(d), units = p.b * p.n_splits;
+  const bool one = p.head_dim == 128 ? p.G <= 8 : p.G <= 4;  // up to eight query heads in a workgroup
   const size_t lds = q8_wide_lds_bytes(cls / 64, cls / 128, one ? 8 : 16);
   if (lds > 160 * 1024 || 2 * p.tiles_per_split > kWideTiles) return LORC_EUNSUPPORTED;
-  return launch_kernel(one ? q8_wide_kernel<1>(cls) : q8_wide_kernel<2>(cls), dim3(((units + 7) / 8) * 8 * nq), dim3(kWideThreads), lds, s, p);
+  return launch_kernel(q8_wide_kernel(p.head_dim, cls, one), dim3(((units + 7) / 8) * 8 * nq), dim3(kWideThreads), lds, s, p);
 }
 
 }  // namespace lorc

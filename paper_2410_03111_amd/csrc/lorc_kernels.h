@@ -181,7 +181,7 @@ int launch_quantize(const QuantizeParams& p, hipStream_t s);
 
 // Decode over 8-bit pages (lorc_decode_q8.hip).  DecodeParams: cache and page_elems are those of the 8-bit pool (page_elems in units of two bytes).
 enum class Q8Form { kRotary, kPlain, kAbsorbed };
-bool q8_shape_ok(const lorc_layer_desc& d, Q8Form form);
+bool q8_shape_ok(const lorc_layer_desc& d, Q8Form form, int max_ctx);
 DecodePlan make_q8_plan(const lorc_layer_desc& d, Q8Form form, int b, int max_ctx, int n_cus, int max_splits);
 DecodePlan make_q8_plan_within(const lorc_layer_desc& d, Q8Form form, int b, int max_ctx, int n_cus, size_t bytes);
 int launch_decode_q8(const lorc_layer_desc& d, Q8Form form, const DecodeParams& p, const DecodePlan& plan, hipStream_t s);
@@ -191,11 +191,11 @@ bool q8_stationary_shape_ok(const lorc_layer_desc& d);
 int q8_stationary_max_tiles();  // pages that a split of it walks at most
 int set_kernel_attributes_decode_q8_stationary();
 int launch_decode_q8_stationary(const DecodeParams& p, hipStream_t s);
-// The same for ranks up to 1024 and any group (lorc_decode_q8_wide.hip).
-bool q8_wide_shape_ok(const lorc_layer_desc& d);
+// The same for every other shape up to rank 1024 (lorc_decode_q8_wide.hip).
+int q8_wide_units(const lorc_layer_desc& d);  // workgroups per (sequence, split)
 int q8_wide_max_tiles();
 int set_kernel_attributes_decode_q8_wide();
-int launch_decode_q8_wide(const DecodeParams& p, hipStream_t s);
+int launch_decode_q8_wide(const lorc_layer_desc& d, const DecodeParams& p, hipStream_t s);
 // Absorbed form up to rank 512 (lorc_decode_q8_abs.hip).
 bool q8_absorbed_shape_ok(const lorc_layer_desc& d);
 int q8_absorbed_max_tiles();

@@ -85,20 +85,20 @@ constexpr size_t kRopeTabBytes = 64 * 8 + 32 * 64 * 8;
 LORC_HD size_t packed_off_rope(int D, int r_k, int r_v, int n) {
   return packed_off_at_tiled(D, r_k, r_v, n) + packed_at_elems(D, r_k, r_v);
 }
-// B_k once more for the decode over 8-bit pages (head_dim 128, key ranks up to 1024): every bf16 entry as the sum of two e4m3 codes under
-// one power of two per column and run of 64 latent indices.  A block is 32 columns of a head, 16 coordinates and their partners: column
-// c of head g is row m = c % 16 + 16 (c / 64) of block 4 g + c % 64 / 16.  Codes [block][run][first, second][i / 2][lane][16]: lane = m +
+// B_k once more for the decode over 8-bit pages (key ranks up to 1024): every bf16 entry as the sum of two e4m3 codes under
+// one power of two per column and run of 64 latent indices.  A block is 32 columns of a head, 16 coordinates and their partners (row m
+// of 32, see below).  Codes [block][run][first, second][i / 2][lane][16]: lane = m +
 // 32 half, byte 8 (i % 2) + e: latent index 64 run + 16 i + 8 half + e (an operand of the fp8 matrix instructions: 1 KiB per load); then the
 // scale bytes (exponent + 127) [block][m][16] of the up to sixteen runs.
 constexpr int kCodedMaxRank = 1024, kCodedMaxSteps = kCodedMaxRank / 64;
-LORC_HD int coded_steps(int head_dim, int r_k) { return head_dim == 128 && r_k <= kCodedMaxRank ? (r_k + 63) / 64 : 0; }
-LORC_HD int coded_block(int c) { return c / 128 * 4 + c % 64 / 16; }
-LORC_HD int coded_row(int c) { return c % 16 + 16 * (c % 128 / 64); }
+LORC_HD int coded_steps(int r_k) { return r_k <= kCodedMaxRank ? (r_k + 63) / 64 : 0; }
+LORC_HD int coded_block(int head_dim, int c) { return c / head_dim * (head_dim / 32) + c % (head_dim / 2) / 16; }
+LORC_HD int coded_row(int head_dim, int c) { return c % 16 + 16 * (c % head_dim / (head_dim / 2)); }
 LORC_HD size_t packed_off_coded_bytes(int D, int r_k, int r_v, int n) {
   return ((packed_off_rope(D, r_k, r_v, n) * 2 + kRopeTabBytes) + 255) & ~(size_t)255;
 }
-LORC_HD size_t packed_total_elems(int D, int r_k, int r_v, int n, int head_dim) {
-  const size_t steps = coded_steps(head_dim, r_k);
+LORC_HD size_t packed_total_elems(int D, int r_k, int r_v, int n) {
+  const size_t steps = coded_steps(r_k);
   if (steps == 0) return packed_off_rope(D, r_k, r_v, n) + kRopeTabBytes / 2;
   return (packed_off_coded_bytes(D, r_k, r_v, n) + steps * n * 128 + (size_t)n * kCodedMaxSteps) / 2;
 }

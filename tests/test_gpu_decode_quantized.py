@@ -152,6 +152,11 @@ SHAPES = {
     "rotary wide keys": dict(form="rotary", h_q=24, h_kv=12, r_k=800, r_v=96),
     "rotary groups of 12": dict(form="rotary", h_q=60, h_kv=5, r_k=416, r_v=448),
     "rotary group of 20": dict(form="rotary", h_q=40, h_kv=2, r_k=224, r_v=32),
+    "rotary d 64, groups of 5, odd kv heads": dict(form="rotary", h_q=15, h_kv=3, d=64, r_k=128, r_v=96),
+    "rotary d 64, groups of 12": dict(form="rotary", h_q=24, h_kv=2, d=64, r_k=64, r_v=128),
+    "rotary d 64, one group of 32": dict(form="rotary", h_q=32, h_kv=1, d=64, r_k=64, r_v=64),
+    "rotary d 64, one head": dict(form="rotary", h_q=1, h_kv=1, d=64, r_k=64, r_v=32),
+    "rotary d 64, rank 1024": dict(form="rotary", h_q=32, h_kv=16, d=64, r_k=1024, r_v=992),
     "rotary d 64, rank 608": dict(form="rotary", h_q=20, h_kv=10, d=64, r_k=608, r_v=576),
 }
 
@@ -161,14 +166,16 @@ def test_lengths(name):
     Cache8(ctx=LENGTHS, **SHAPES[name]).check()
 
 
-@pytest.mark.parametrize("name", ["plain 8b", "plain groups of 20", "absorbed 8b", "absorbed 64 heads", "rotary 8b", "rotary 70b", "rotary uneven", "rotary rank 1024", "rotary rank 768, 64 heads", "rotary groups of 12"])
+@pytest.mark.parametrize("name", ["plain 8b", "plain groups of 20", "absorbed 8b", "absorbed 64 heads", "rotary 8b", "rotary 70b", "rotary uneven", "rotary rank 1024", "rotary rank 768, 64 heads", "rotary groups of 12",
+                                  "rotary d 64", "rotary d 64, groups of 5, odd kv heads", "absorbed rank 1024"])
 @pytest.mark.parametrize("ctx", [[3001], [1, 2500, 700, 1337]])
 def test_longer_contexts(name, ctx):
     Cache8(ctx=ctx, seed=11, **SHAPES[name]).check()
 
 
 FORMS = {"plain": dict(form="plain", h_q=8, h_kv=2), "absorbed": dict(form="absorbed", h_q=8, h_kv=2, r_k=160, r_v=128),
-         "rotary": dict(form="rotary", h_q=8, h_kv=2, r_k=192, r_v=256), "rotary wide": dict(form="rotary", h_q=24, h_kv=2, r_k=160, r_v=192), "rotary any": dict(form="rotary", h_q=6, h_kv=3, d=64, r_k=64, r_v=96)}
+         "absorbed wide": dict(form="absorbed", h_q=10, h_kv=5, r_k=64, r_v=544),
+         "rotary": dict(form="rotary", h_q=8, h_kv=2, r_k=192, r_v=256), "rotary wide": dict(form="rotary", h_q=24, h_kv=2, r_k=160, r_v=192), "rotary d 64": dict(form="rotary", h_q=6, h_kv=3, d=64, r_k=64, r_v=96)}
 
 
 @pytest.mark.parametrize("name", FORMS)

@@ -128,3 +128,17 @@ def test_a_workspace_for_a_larger_call_holds_one_split_of_every_smaller_one(name
         least = b * 32 * 8 + b * 32 * width * 2
         assert all(size(d, b2, ctx2) >= least for b2 in (b, b + 1, 2 * b) for ctx2 in (ctx, ctx + 65, 2 * ctx + 4096))
         assert size(d, b, -1) == 0 and size(d, 0, ctx) == 0
+
+
+@pytest.mark.parametrize("name", FORMS)
+def test_contexts_beyond_what_512_splits_walk_are_refused(name):
+    rotary, size, d = FORMS[name]
+    most = {True: 512 * 128 * 64, False: 1 << 30}["_attention_quantized" in name]   # a rotary split walks up to 128 pages
+    if "absorbed" in name:
+        most = 512 * 1024 * 64
+    args = dict(desc=ctypes.byref(d), q=P, **(dict(q_pos=P) if rotary else {}), ctx_len=P, b=1, max_ctx=0, packed=P, cache=P, block_table=P, max_pages=1 << 25, n_pages=9,
+                out=P, workspace=P, workspace_bytes=1 << 40)
+    assert size(d, 1, most) > 0
+    for ctx in (most + 1, 2 ** 31 - 64, 2 ** 31 - 1):
+        assert size(d, 1, ctx) == 0
+        assert getattr(lib, name)(*{**args, "max_ctx": ctx}.values(), None) == L.EUNSUPPORTED
