@@ -509,6 +509,8 @@ def copy_pages(pool, src, dst, page_bytes=None):
     _same_length(n, ("dst",), dst)
     total = pool.numel() * pool.element_size()
     if page_bytes is None:
+        if pool.dim() < 1 or total == 0:
+            raise ValueError(f"pool: no pages in a tensor of shape {tuple(pool.shape)}")
         page_bytes = total // pool.shape[0]
     _check(_lib.lorc_copy_pages(pool.data_ptr(), page_bytes, total // page_bytes if page_bytes > 0 else 0, src.data_ptr(), dst.data_ptr(), n,
                                 torch._C._cuda_getCurrentRawStream(dev)), "lorc_copy_pages")
@@ -644,6 +646,8 @@ def _decode_quantized(name, call, size, desc, q, width, q_pos, ctx_len, max_ctx,
     page = page_bytes_quantized(desc)
     if page == 0:
         raise LorcError(EUNSUPPORTED, "lorc_page_bytes_quantized")
+    if packed.numel() < packed_bytes(desc):
+        raise ValueError(f"packed: {packed.numel()} bytes, expected {packed_bytes(desc)}")
     query = (q.data_ptr(),) if q_pos is None else (q.data_ptr(), q_pos.data_ptr())
     _check(call(ctypes.byref(desc), *query, ctx_len.data_ptr(), b, max_ctx, packed.data_ptr(), cache.data_ptr(), block_table.data_ptr(),
                 rows_max[1], cache.numel() // page, out.data_ptr(), workspace.data_ptr(), workspace.numel(),

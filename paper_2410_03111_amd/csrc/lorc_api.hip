@@ -396,9 +396,12 @@ int lorc_prefill_attention_plain(const lorc_layer_desc* desc, const void* q, con
 // ---- pages
 namespace {
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+constexpr int kMostEntries = 1 << 30;  // of tables, counts and lists: what a plan adds up and steps over stays below 2^31
+bool list_ok(int32_t n) { return n >= 0 && n <= kMostEntries; }
 int table_args(const void* block_table, int32_t n_seqs, int32_t max_pages, const void* page_refs, int32_t n_pages) {
   if (!block_table || !page_refs || n_seqs <= 0 || max_pages <= 0 || n_pages <= 0) return LORC_EINVAL;
-  return max_pages > INT32_MAX / kPage ? LORC_EINVAL : LORC_OK;
+  if (max_pages > INT32_MAX / kPage || (long)n_seqs * max_pages > kMostEntries || n_pages > kMostEntries) return LORC_EINVAL;
+  return LORC_OK;
 }
 }  // namespace
 
@@ -417,7 +420,7 @@ int lorc_fork_sequences(int32_t* block_table, int32_t n_seqs, int32_t max_pages,
                         const int32_t* parents, const int32_t* children, const int32_t* lens, int32_t n, int32_t* copy_src,
                         int32_t* copy_dst, int32_t* status, void* workspace, size_t workspace_bytes, void* stream) {
   if (int rc = table_args(block_table, n_seqs, max_pages, page_refs, n_pages)) return rc;
-  if (!parents || !children || !lens || !copy_src || !copy_dst || !status || !workspace || n < 0) return LORC_EINVAL;
+  if (!parents || !children || !lens || !copy_src || !copy_dst || !status || !workspace || !list_ok(n)) return LORC_EINVAL;
   if (reinterpret_cast<uintptr_t>(workspace) & 255) return LORC_EINVAL;
   if (workspace_bytes < lorc_pages_workspace_bytes(n_seqs, n_pages)) return LORC_EWORKSPACE;
   if (n == 0) return LORC_OK;
@@ -442,7 +445,7 @@ int lorc_fork_sequences(int32_t* block_table, int32_t n_seqs, int32_t max_pages,
 int lorc_free_sequences(int32_t* block_table, int32_t n_seqs, int32_t max_pages, int32_t* page_refs, int32_t n_pages,
                         const int32_t* seqs, int32_t n, void* stream) {
   if (int rc = table_args(block_table, n_seqs, max_pages, page_refs, n_pages)) return rc;
-  if (!seqs || n < 0) return LORC_EINVAL;
+  if (!seqs || !list_ok(n)) return LORC_EINVAL;
   if (n == 0) return LORC_OK;
   return launch_free(block_table, n_seqs, max_pages, page_refs, n_pages, seqs, n, static_cast<hipStream_t>(stream));
 }
@@ -450,7 +453,7 @@ int lorc_free_sequences(int32_t* block_table, int32_t n_seqs, int32_t max_pages,
 int lorc_compact_pages(int32_t* block_table, int32_t n_seqs, int32_t max_pages, int32_t* page_refs, int32_t n_pages,
                        int32_t* move_src, int32_t* move_dst, int32_t max_moves, int32_t* page_map, void* stream) {
   if (int rc = table_args(block_table, n_seqs, max_pages, page_refs, n_pages)) return rc;
-  if (!page_map || max_moves < 0 || (max_moves > 0 && (!move_src || !move_dst))) return LORC_EINVAL;
+  if (!page_map || !list_ok(max_moves) || (max_moves > 0 && (!move_src || !move_dst))) return LORC_EINVAL;
   CompactParams p;
   p.block_table = block_table;
   p.page_refs = page_refs;
@@ -468,7 +471,7 @@ int lorc_reserve_pages(int32_t* block_table, int32_t n_seqs, int32_t max_pages, 
                        const int32_t* seqs, const int32_t* lens, int32_t n, int32_t* status, void* workspace,
                        size_t workspace_bytes, void* stream) {
   if (int rc = table_args(block_table, n_seqs, max_pages, page_refs, n_pages)) return rc;
-  if (!seqs || !lens || !status || !workspace || n < 0) return LORC_EINVAL;
+  if (!seqs || !lens || !status || !workspace || !list_ok(n)) return LORC_EINVAL;
   if (reinterpret_cast<uintptr_t>(workspace) & 255) return LORC_EINVAL;
   if (workspace_bytes < lorc_pages_workspace_bytes(n_seqs, n_pages)) return LORC_EWORKSPACE;
   if (n == 0) return LORC_OK;
@@ -496,6 +499,7 @@ int lorc_quantize_latents(const lorc_layer_desc* desc, const void* cache, const 
   if (!desc || !cache || !block_table || !pos_begin || !pos_end || !cache_q8 || !block_table_q8) return LORC_EINVAL;
   if (int rc = check_desc(*desc)) return rc;
   if (b <= 0 || max_tokens < 0 || max_pages <= 0 || n_pages <= 0 || max_pages_q8 <= 0 || n_pages_q8 <= 0) return LORC_EINVAL;
+  if (max_pages > INT32_MAX / kPage || max_pages_q8 > INT32_MAX / kPage) return LORC_EINVAL;
   if (!aligned16(cache) || !aligned16(cache_q8)) return LORC_EINVAL;
   if (max_tokens == 0) return LORC_OK;
   QuantizeParams p;

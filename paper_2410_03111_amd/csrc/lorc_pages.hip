@@ -427,7 +427,6 @@ int launch_free(int32_t* block_table, int n_seqs, int max_pages, int32_t* page_r
 int launch_compact(const CompactParams& p, hipStream_t s) {
   const size_t entries = (size_t)p.n_seqs * p.max_pages;
   const bool rename = entries <= kSmallTable;
-  if (entries > (size_t)0x7fffffff * 256) return LORC_EINVAL;
   if (int rc = launch_kernel(rename ? compact_plan_kernel<true> : compact_plan_kernel<false>, dim3(1), dim3(kPlanThreads), 0, s, p)) return rc;
   if (rename) return LORC_OK;
   return launch_kernel(rename_pages_kernel, dim3((uint32_t)((entries + 255) / 256)), dim3(256), 0, s, p.block_table, entries, p.page_map, p.n_pages);

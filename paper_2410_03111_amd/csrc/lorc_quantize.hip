@@ -39,10 +39,10 @@ __global__ __launch_bounds__(256) void quantize_latents_kernel(QuantizeParams p)
   if (unit >= units) return;
   int begin = p.pos_begin[seq], end = p.pos_end[seq];
   if (begin < 0) begin = 0;
+  if (end <= begin) return;
   if (end - begin > p.max_tokens) end = begin + p.max_tokens;
   const int page = begin / kPage + nth;
-  if (end <= page * kPage || end <= begin) return;
-  if (page >= p.src_max_pages || page >= p.dst_max_pages) return;
+  if (page >= p.src_max_pages || page >= p.dst_max_pages || end <= page * kPage) return;
   const int from = __builtin_amdgcn_readfirstlane(p.src_table[(size_t)seq * p.src_max_pages + page]);
   const int to = __builtin_amdgcn_readfirstlane(p.dst_table[(size_t)seq * p.dst_max_pages + page]);
   if (from < 0 || from >= p.src_pages || to < 0 || to >= p.dst_pages) return;

@@ -315,6 +315,43 @@ def test_replays_from_a_graph_on_another_stream(name):
         assert torch.equal(got, out) and bool(torch.isfinite(got).all()), rep
 
 
+@pytest.mark.parametrize("name", ["plain", "absorbed", "rotary"])
+def test_rows_of_the_table_behind_the_batch_and_refused_arguments(name):
+    import torch
+    c = Cache8(ctx=[70, 130], seed=17, **FORMS[name])
+    L = c.L
+    want = c.call()
+    out = torch.full((3, c.h_q, c.d), 7.0, dtype=torch.bfloat16, device="cuda")
+    c.block_table = torch.cat([c.block_table, torch.full_like(c.block_table[:1], 0)])       # a third row that no sequence has
+    c.call(out=out[:2])
+    assert torch.equal(out[:2], want) and bool((out[2] == 7.0).all())
+    fn = {"plain": L.decode_attention_plain_quantized, "absorbed": L.decode_attention_absorbed_quantized, "rotary": L.decode_attention_quantized}[name]
+    ctx, pos = c.i32(c.ctx), c.i32([69, 129])
+    q, first = ("q_lat", {}) if name == "absorbed" else ("q", dict(q_pos=pos))
+    good = {"desc": c.desc, q: c.dq, **first, "ctx_len": ctx, "max_ctx": 130, "packed": c.packed, "cache_q8": c.pool, "block_table": c.block_table}
+    assert torch.equal(fn(**good), want)
+    bad = [(q, c.dq.float(), TypeError), (q, c.dq[:, ::2], TypeError), (q, c.dq[:, :1].contiguous(), ValueError), ("ctx_len", ctx[:1], ValueError),
+           ("ctx_len", ctx.to(torch.int64), TypeError), ("packed", c.packed[:64], ValueError), ("packed", c.packed.cpu(), TypeError), ("cache_q8", c.pool[:10], L.LorcError),
+           ("block_table", c.block_table[:1], ValueError), ("block_table", c.block_table[:, ::2], TypeError), ("max_ctx", 10 ** 6, L.LorcError), ("max_ctx", -1, L.LorcError),
+           ("out", out, ValueError), ("out", out[:2].float(), TypeError), ("workspace", torch.zeros(64, dtype=torch.uint8, device="cuda"), L.LorcError)]
+    if first:
+        bad += [("q_pos", pos[:1], ValueError), ("q_pos", pos.cpu(), TypeError)]
+    for key, value, error in bad:
+        with pytest.raises(error):
+            fn(**{**good, key: value})
+
+
+@pytest.mark.parametrize("name", FORMS)
+def test_a_query_of_nan_stays_in_its_head(name):
+    c = Cache8(ctx=[300, 65], seed=18, **FORMS[name])
+    want = c.call().float().cpu().numpy()
+    c.dq[0, 1] = float("nan")
+    got = c.call().float().cpu().numpy()
+    assert np.all(np.isnan(got[0, 1]))
+    got[0, 1] = want[0, 1]
+    assert np.array_equal(got, want)
+
+
 def test_a_served_prompt_from_prefill_to_its_forks():
     """Append, prefill, into the 8-bit cache, three answers that share the prompt's pages, decode steps of their own, a finished one
     released, the pool made dense under the others: every step against fp64 on the values that the pages stand for."""

@@ -205,3 +205,64 @@ def test_calls_replay_from_a_graph_on_another_stream():
         torch.cuda.synchronize()
         for a, b in zip(results(), eager):
             assert np.array_equal(a, b), rep
+
+
+def test_refused_arguments():
+    import torch
+    import paper_2410_03111_amd as L
+    table, refs, row, other = dev32(np.full((4, 3), -1)), dev32(np.zeros(9)), dev32([0, 1]), dev32([2, 3])
+    src, dst, status = dev32([0, 0]), dev32([0, 0]), dev32([0, 0])
+    ws = torch.empty(L.pages_workspace_bytes(4, 9), dtype=torch.uint8, device="cuda")
+    good = {L.fork_sequences: dict(block_table=table, page_refs=refs, parents=row, children=other, lens=row, copy_src=src, copy_dst=dst, status=status, workspace=ws),
+            L.free_sequences: dict(block_table=table, page_refs=refs, seqs=row),
+            L.compact_pages: dict(block_table=table, page_refs=refs, move_src=src, move_dst=dst, page_map=dev32(np.zeros(9))),
+            L.reserve_pages: dict(block_table=table, page_refs=refs, seqs=row, lens=row, status=status, workspace=ws)}
+    for call, args in good.items():
+        call(**args)
+        for key, t in args.items():
+            wide = torch.zeros(t.shape[0] * 2, *t.shape[1:], dtype=t.dtype, device="cuda")
+            for bad in (t.cpu(), t.to(torch.int64), wide[::2], None if key != "workspace" else 5):
+                with pytest.raises(TypeError):
+                    call(**{**args, key: bad})
+            if key not in ("block_table", "page_refs", "seqs", "parents", "workspace", "move_src"):
+                with pytest.raises(ValueError):
+                    call(**{**args, key: wide})
+        if "workspace" in args:
+            with pytest.raises(L.LorcError):
+                call(**{**args, "workspace": ws[:-1]})
+    pool = torch.zeros(9, 32, dtype=torch.uint8, device="cuda")
+    L.copy_pages(pool, row, other)
+    for bad, error in ((dict(pool=pool.cpu()), TypeError), (dict(pool=pool[:, ::2]), TypeError), (dict(src=row.to(torch.int64)), TypeError), (dict(dst=other[:1]), ValueError),
+                       (dict(pool=pool[:0]), ValueError), (dict(page_bytes=24), L.LorcError), (dict(page_bytes=0), L.LorcError), (dict(page_bytes=-16), L.LorcError),
+                       (dict(page_bytes=512), L.LorcError), (dict(pool=pool.view(-1)[8:-24].view(8, 32)), L.LorcError)):
+        with pytest.raises(error):
+            L.copy_pages(**{**dict(pool=pool, src=row, dst=other), **bad})
+
+
+def test_two_graphs_share_a_workspace():
+    import torch
+    import paper_2410_03111_amd as L
+    ws = torch.empty(L.pages_workspace_bytes(5000, 700), dtype=torch.uint8, device="cuda")      # a table beyond what a small plan holds
+    rng, graphs, pools = np.random.default_rng(3), [], []
+    for g in range(2):
+        pool = Pool(5000, 4, 700)
+        rows = rng.permutation(5000)[:120]
+        pool.reserve(rows, rng.integers(0, 257, 120))
+        args = rows[:40], np.setdiff1d(np.arange(5000), rows)[:40], rng.integers(0, 257, 40)
+        lists = [dev32(a) for a in args] + [dev32(np.full(40, 77)) for _ in range(3)]
+        keep = pool.table.clone(), pool.refs.clone()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            pool.table.copy_(keep[0]), pool.refs.copy_(keep[1])
+            L.fork_sequences(pool.table, pool.refs, *lists, workspace=ws)
+        want = pool.o.fork(*[list(map(int, a)) for a in args])
+        graphs.append(graph)
+        pools.append((pool, lists, want, keep))
+    for rep in range(3):
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for pool, lists, want, _ in pools:
+            pool.same(rep)
+            assert [t.cpu().tolist() for t in lists[3:]] == [list(w) for w in want]
+        ws.fill_(255)

@@ -82,6 +82,31 @@ def test_longer_ranges_are_cut_off():
     assert np.array_equal(got, want)
 
 
+def test_ranges_at_the_ends_of_int32():
+    table = ids(4, 3, 6)
+    got, want = run(latents(12, 64 + 32, 7), 64, 32, [5, 2 ** 31 - 1, -2 ** 31, 3], [-2 ** 31, 2 ** 31 - 1, 2, 2 ** 31 - 1], max_tokens=250, table=table)
+    assert np.array_equal(got, want)
+
+
+def test_no_rows_behind_the_last_sequence_and_refused_arguments():
+    import torch
+    import paper_2410_03111_amd as L
+    d = layer(64, 32)
+    size, size_q8 = L.page_bytes(d), L.page_bytes_quantized(d)
+    cache, got = torch.zeros(4 * size, dtype=torch.uint8, device="cuda"), torch.full((4 * size_q8,), 9, dtype=torch.uint8, device="cuda")
+    table = torch.tensor([[0], [1], [2]], dtype=torch.int32, device="cuda")
+    begin, end = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.full((2,), 64, dtype=torch.int32, device="cuda")
+    L.quantize_latents(d, cache, table, begin, end, 64, got, table)                 # a table of three rows, two sequences
+    assert not bool((got[:2 * size_q8] == 9).any()) and bool((got[2 * size_q8:] == 9).all())
+    good = dict(cache=cache, block_table=table, pos_begin=begin, pos_end=end, max_tokens=64, cache_q8=got, block_table_q8=table)
+    for key, value, error in (("cache", cache.cpu(), TypeError), ("cache", cache.to(torch.int16), TypeError), ("cache_q8", got[::2], TypeError),
+                              ("block_table", table.to(torch.int64), TypeError), ("block_table", table[:1], ValueError),
+                              ("block_table_q8", table[:1], ValueError), ("pos_end", end[:1], ValueError), ("pos_begin", [0, 0], TypeError),
+                              ("max_tokens", -1, L.LorcError), ("cache", cache[:100], L.LorcError), ("cache_q8", got[8:], L.LorcError)):
+        with pytest.raises(error):
+            L.quantize_latents(d, **{**good, key: value})
+
+
 def test_unmapped_pages_and_tables_of_different_width():
     table, table_q8 = ids(2, 3, 3), ids(2, 3, 4)[:, :2].copy()
     table[0, 1], table_q8[1, 0] = -1, 6

@@ -142,3 +142,22 @@ def test_contexts_beyond_what_512_splits_walk_are_refused(name):
     for ctx in (most + 1, 2 ** 31 - 64, 2 ** 31 - 1):
         assert size(d, 1, ctx) == 0
         assert getattr(lib, name)(*{**args, "max_ctx": ctx}.values(), None) == L.EUNSUPPORTED
+
+
+def test_tables_counts_and_lists_beyond_2_to_the_30_are_refused():
+    table = dict(block_table=P, n_seqs=4, max_pages=8, page_refs=P, n_pages=100)
+    for name, args, count in (("lorc_fork_sequences", dict(parents=P, children=P, lens=P, n=0, copy_src=P, copy_dst=P, status=P, workspace=P, workspace_bytes=1 << 40), "n"),
+                              ("lorc_free_sequences", dict(seqs=P, n=0), "n"),
+                              ("lorc_compact_pages", dict(move_src=P, move_dst=P, max_moves=0, page_map=P), "max_moves"),
+                              ("lorc_reserve_pages", dict(seqs=P, lens=P, n=0, status=P, workspace=P, workspace_bytes=1 << 40), "n")):
+        for bad in (dict(n_pages=(1 << 30) + 1), dict(n_seqs=(1 << 30) // 8 + 1), dict(n_seqs=2 ** 31 - 1), {count: (1 << 30) + 1}):
+            assert getattr(lib, name)(*{**table, **args, **bad}.values(), None) == L.EINVAL, (name, bad)
+
+
+@pytest.mark.parametrize("which", ["max_pages", "max_pages_q8"])
+def test_positions_of_a_quantized_table_stay_below_2_to_the_31(which):
+    d = desc()
+    args = dict(desc=ctypes.byref(d), cache=P, block_table=P, max_pages=4, n_pages=9, pos_begin=P, pos_end=P, b=2, max_tokens=0, cache_q8=P,
+                block_table_q8=P, max_pages_q8=4, n_pages_q8=9)
+    assert lib.lorc_quantize_latents(*args.values(), None) == L.OK
+    assert lib.lorc_quantize_latents(*{**args, which: 1 << 25}.values(), None) == L.EINVAL
