@@ -33,12 +33,11 @@ __device__ __forceinline__ int wave_inclusive(int v) {
   return v;
 }
 
-// Exclusive prefix sum over the workgroup's threads; *total: the sum.  `sums`: kPlanWaves words of LDS.
-__device__ __forceinline__ int block_exclusive(int v, int* sums, int* total) {
+// Sum over the waves before this one of a wave's v; *total: over all of them.  `sums`: kPlanWaves words of LDS.
+__device__ __forceinline__ int waves_exclusive(int v, int* sums, int* total) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int inc = wave_inclusive(v);
   __syncthreads();  // the words may still be read from the call before
-  if (lane == 63) sums[w] = inc;
+  if (lane == 63) sums[w] = v;
   __syncthreads();
   int before = 0, all = 0;
 #pragma unroll
@@ -48,46 +47,76 @@ __device__ __forceinline__ int block_exclusive(int v, int* sums, int* total) {
     all += s;
   }
   *total = all;
-  return before + inc - v;
+  return before;
 }
 
-// The counts of up to 16 consecutive pages from `first` on, as a mask of those that are free (bit set) and how many are there.
-__device__ __forceinline__ uint32_t free_mask(const int* refs, int first, int n_pages) {
-  uint32_t mask = 0;
-  if (first + kPerThread <= n_pages && (reinterpret_cast<uintptr_t>(refs) & 15) == 0) {
+// Exclusive prefix sum over the workgroup's threads; *total: the sum.
+__device__ __forceinline__ int block_exclusive(int v, int* sums, int* total) {
+  const int inc = wave_inclusive(v);
+  return waves_exclusive(inc, sums, total) + inc - v;
+}
+
+__device__ __forceinline__ uint64_t lanes_below(int n) { return n <= 0 ? 0 : n >= 64 ? ~(uint64_t)0 : ((uint64_t)1 << n) - 1; }
+
+// A pass over up to kStep pages: every wave walks `chunks` times 64 neighbours and keeps a bit for each page in scalar registers.  (Two other
+// ways: a thread with sixteen neighbours of its own touches a cache line per lane with every load; sixteen chunks whatever the pool's
+// size cost 5 us more, because what bounds a plan is its instructions: one compute unit runs them for all sixteen waves.)
+struct Pages {
+  uint64_t bits[kPerThread];
+  int base, chunks;
+  __device__ __forceinline__ int page(int u) const { return base + ((int)(threadIdx.x >> 6) * chunks + u) * 64 + (int)(threadIdx.x & 63); }
+  __device__ __forceinline__ int first(int u) const { return base + (__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) * chunks + u) * 64; }
+};
+__device__ __forceinline__ Pages pass_at(int base, int n_pages) {
+  Pages f;
+  const int chunks = (n_pages - base + kPlanThreads - 1) / kPlanThreads;
+  f.base = base;
+  f.chunks = chunks < kPerThread ? chunks : kPerThread;
+  return f;
+}
+__device__ __forceinline__ Pages free_pages(const int* refs, int base, int n_pages) {
+  Pages f = pass_at(base, n_pages);
+  int v[kPerThread];
 #pragma unroll
-    for (int u = 0; u < kPerThread / 4; ++u) {
-      const int4 v = *reinterpret_cast<const int4*>(refs + first + 4 * u);
-      mask |= (v.x <= 0 ? 1u : 0u) << (4 * u) | (v.y <= 0 ? 2u : 0u) << (4 * u) | (v.z <= 0 ? 4u : 0u) << (4 * u) | (v.w <= 0 ? 8u : 0u) << (4 * u);
-    }
-  } else {
-    for (int u = 0; u < kPerThread; ++u)
-      if (first + u < n_pages && refs[first + u] <= 0) mask |= 1u << u;
+  for (int u = 0; u < kPerThread; ++u)
+    if (u < f.chunks) v[u] = f.page(u) < n_pages ? refs[f.page(u)] : 1;
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u) f.bits[u] = u < f.chunks ? __ballot(v[u] <= 0) : 0;
+  return f;
+}
+// The pages of a pass from `page` on are cleared.
+__device__ __forceinline__ void keep_below(Pages& f, int page) {
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u)
+    if (u < f.chunks) f.bits[u] &= lanes_below(page - f.first(u));
+}
+// emit(rank, page) for every page of the pass, ranks ascending from `seen`; returns how many there are.
+template <typename F>
+__device__ __forceinline__ int each_page(const Pages& f, int seen, int* sums, F emit) {
+  int count = 0, total;
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u) count += __popcll(f.bits[u]);
+  int rank = seen + waves_exclusive(count, sums, &total);
+  const uint64_t lower = lanes_below(threadIdx.x & 63);
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u) {
+    if (f.bits[u] == 0) continue;
+    if (f.bits[u] >> (threadIdx.x & 63) & 1) emit(rank + __popcll(f.bits[u] & lower), f.page(u));
+    rank += __popcll(f.bits[u]);
   }
-  return mask;
+  return total;
 }
 
 // emit(k, page) for the free pages of rank k < want, in ascending order; returns how many free pages there are among those walked
-// (all of them where fewer than `want` exist).  first_mask: free_mask of the thread's first 16 pages, asked for early.
+// (all of them where fewer than `want` exist).  first: the first pass, asked for early.
 template <typename F>
-__device__ __forceinline__ int each_free(const int* refs, int n_pages, uint32_t first_mask, int want, int* sums, F emit) {
+__device__ __forceinline__ int each_free(const int* refs, int n_pages, const Pages& first, int want, int* sums, F emit) {
   int seen = 0;
-  for (int base = 0; base < n_pages && seen < want; base += kStep) {
-    const int first = base + (int)threadIdx.x * kPerThread;
-    uint32_t mask = base == 0 ? first_mask : first < n_pages ? free_mask(refs, first, n_pages) : 0u;
-    int total;
-    int rank = seen + block_exclusive(__popc(mask), sums, &total);
-    while (mask != 0 && rank < want) {
-      emit(rank++, first + __ffs(mask) - 1);
-      mask &= mask - 1;
-    }
-    seen += total;
-  }
+  for (int base = 0; base < n_pages && seen < want; base += kStep)
+    seen += each_page(base == 0 ? first : free_pages(refs, base, n_pages), seen, sums, [&](int k, int page) {
+      if (k < want) emit(k, page);
+    });
   return seen;
-}
-__device__ __forceinline__ uint32_t first_free_mask(const int* refs, int n_pages) {
-  const int first = (int)threadIdx.x * kPerThread;
-  return first < n_pages ? free_mask(refs, first, n_pages) : 0u;
 }
 // Words that pass between the threads of a plan: in LDS, or in the workspace.
 template <bool LDS>
@@ -134,11 +163,11 @@ __global__ __launch_bounds__(256) void copy_pages_kernel(unsigned char* pool, si
 }
 
 // ------------------------------------------------------------------------------------------------ fork
-// One wave: the child's row, and the counts of the pages that it shares.
-__device__ __forceinline__ void fork_row(const ForkParams& p, int parent, int child, int len, int fresh) {
+// One wave, or `waves` of them: the child's row, and the counts of the pages that it shares.
+__device__ __forceinline__ void fork_row(const ForkParams& p, int parent, int child, int len, int fresh, int wave = 0, int waves = 1) {
   const int whole = len / kPage, *from = p.block_table + (size_t)parent * p.max_pages;
   int* to = p.block_table + (size_t)child * p.max_pages;
-  for (int e = threadIdx.x & 63; e < p.max_pages; e += 64) {
+  for (int e = 64 * wave + (int)(threadIdx.x & 63); e < p.max_pages; e += 64 * waves) {
     int id = e < whole ? from[e] : e == whole ? fresh : -1;
     if (!maps(id, p.n_pages)) id = -1;
     else if (e < whole) atomicAdd(p.page_refs + id, 1);
@@ -155,7 +184,7 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(ForkParams p) {
   int* owner = SMALL ? owner_lds : p.owner;
   int* asks = SMALL ? asks_lds : p.asks;
   const int tid = threadIdx.x;
-  const uint32_t first_mask = first_free_mask(p.page_refs, p.n_pages);
+  const Pages first_pass = free_pages(p.page_refs, 0, p.n_pages);
   for (int s = tid; s < p.n_seqs; s += kPlanThreads) put<SMALL>(owner + s, INT_MAX);
   const long most = (long)p.max_pages * kPage;
   auto named = [&](int i, int& parent, int& child, int& len) {
@@ -194,7 +223,7 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(ForkParams p) {
     }
   }
   plan_barrier();
-  const int found = each_free(p.page_refs, p.n_pages, first_mask, asked, sums, [&](int k, int page) {
+  const int found = each_free(p.page_refs, p.n_pages, first_pass, asked, sums, [&](int k, int page) {
     const int i = get<SMALL>(asks + k);
     p.copy_dst[i] = page;
     p.status[i] = LORC_PAGES_OK;
@@ -208,22 +237,23 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(ForkParams p) {
   }
 }
 
-__global__ __launch_bounds__(256) void fork_rows_kernel(ForkParams p) {
-  const int i = blockIdx.x * 4 + (int)(threadIdx.x >> 6);
-  if (i >= p.n || p.status[i] != LORC_PAGES_OK) return;
-  fork_row(p, p.parents[i], p.children[i], p.lens[i], p.copy_dst[i]);
+__global__ __launch_bounds__(256) void fork_rows_kernel(ForkParams p, int waves) {
+  const int at = blockIdx.x * 4 + (int)(threadIdx.x >> 6), i = at / waves;
+  if (i >= p.n) return;
+  const int status = p.status[i], parent = p.parents[i], child = p.children[i], len = p.lens[i], fresh = p.copy_dst[i];
+  if (status == LORC_PAGES_OK) fork_row(p, parent, child, len, fresh, at % waves, waves);
 }
 
 // ------------------------------------------------------------------------------------------------ free
-// One wave per row.  An entry is claimed by an exchange, so that a row named twice is released once.
+// `waves` waves per row.  An entry is claimed by an exchange, so that a row named twice is released once.
 __global__ __launch_bounds__(256) void free_rows_kernel(int* block_table, int n_seqs, int max_pages, int* page_refs, int n_pages,
-                                                        const int* __restrict__ seqs, int n) {
-  const int i = blockIdx.x * 4 + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
+                                                        const int* __restrict__ seqs, int n, int waves) {
+  const int at = blockIdx.x * 4 + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63, i = at / waves;
   if (i >= n) return;
   const int s = seqs[i];
   if (s < 0 || s >= n_seqs) return;
   int* row = block_table + (size_t)s * max_pages;
-  for (int e = lane; e < max_pages; e += 64) {
+  for (int e = 64 * (at % waves) + lane; e < max_pages; e += 64 * waves) {
     const int id = atomicExch(row + e, -1);
     if (maps(id, n_pages)) atomicSub(page_refs + id, 1);
   }
@@ -236,44 +266,32 @@ template <bool RENAME>
 __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(CompactParams p) {
   __shared__ int sums[kPlanWaves];
   const int tid = threadIdx.x;
-  const uint32_t first_mask = first_free_mask(p.page_refs, p.n_pages);
-  auto mask_of = [&](int base) {
-    const int first = base + tid * kPerThread;
-    return base == 0 ? first_mask : first < p.n_pages ? free_mask(p.page_refs, first, p.n_pages) : 0u;
-  };
   int n_free = 0;
-  for (int base = 0; base < p.n_pages; base += kStep) {
-    int total;
-    block_exclusive(__popc(mask_of(base)), sums, &total);
-    n_free += total;
-  }
+  for (int base = 0; base < p.n_pages; base += kStep) n_free += each_page(free_pages(p.page_refs, base, p.n_pages), 0, sums, [](int, int) {});
   const int used = p.n_pages - n_free;
   int holes = 0;  // free pages below `used`: as many as used pages from there on
   for (int base = 0; base < used; base += kStep) {
-    const int first = base + tid * kPerThread, n_here = used - first;
-    uint32_t mask = mask_of(base);
-    if (n_here < kPerThread) mask &= n_here <= 0 ? 0u : (1u << n_here) - 1u;
-    int total;
-    int rank = holes + block_exclusive(__popc(mask), sums, &total);
-    for (uint32_t m = mask; m != 0; m &= m - 1, ++rank)
-      if (rank < p.max_moves) store_fresh(p.move_dst + rank, first + __ffs(m) - 1);
-    holes += total;
+    Pages f = free_pages(p.page_refs, base, p.n_pages);
+    keep_below(f, used);
+    holes += each_page(f, holes, sums, [&](int k, int page) {
+      if (k < p.max_moves) store_fresh(p.move_dst + k, page);
+    });
   }
   const int moves = holes < p.max_moves ? holes : p.max_moves;
   for (int k = moves + tid; k < p.max_moves; k += kPlanThreads) p.move_src[k] = p.move_dst[k] = -1;
   for (int id = tid; id < p.n_pages; id += kPlanThreads) store_fresh(p.page_map + id, id);
-  int rest = holes;  // used pages not yet walked
+  int walked = 0;  // used pages from `used` on
   for (int base = used / kStep * kStep; base < p.n_pages; base += kStep) {
-    const int first = base + tid * kPerThread;
-    int n_here = p.n_pages - first, skip = used - first;  // pages [skip, n_here) of the thread's count
-    n_here = n_here < 0 ? 0 : (n_here > kPerThread ? kPerThread : n_here);
-    skip = skip < 0 ? 0 : (skip > n_here ? n_here : skip);
-    const uint32_t mask = ~mask_of(base) & ((1u << n_here) - 1u) & ~((1u << skip) - 1u);
-    int total;
-    int k = rest - 1 - block_exclusive(__popc(mask), sums, &total);  // rank from the top
-    for (uint32_t m = mask; m != 0; m &= m - 1, --k)
-      if (k < moves) store_fresh(p.move_src + k, first + __ffs(m) - 1);
-    rest -= total;
+    Pages f = free_pages(p.page_refs, base, p.n_pages), below = f;
+#pragma unroll
+    for (int u = 0; u < kPerThread; ++u) f.bits[u] = below.bits[u] = u < f.chunks ? ~f.bits[u] : 0;
+    keep_below(f, p.n_pages);
+    keep_below(below, used);
+#pragma unroll
+    for (int u = 0; u < kPerThread; ++u) f.bits[u] &= ~below.bits[u];
+    walked += each_page(f, walked, sums, [&](int k, int page) {
+      if (holes - 1 - k < moves) store_fresh(p.move_src + holes - 1 - k, page);  // rank from the top
+    });
   }
   plan_barrier();
   for (int k = tid; k < moves; k += kPlanThreads) {
@@ -293,6 +311,73 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(CompactParam
   }
 }
 
+// The same for pools of up to kStep pages: one pass, whose counts stay in registers; moves and the map pass through LDS.
+template <bool RENAME>
+__global__ __launch_bounds__(kPlanThreads) void compact_small_kernel(CompactParams p) {
+  __shared__ int sums[kPlanWaves];
+  __shared__ uint16_t dst_of[kStep / 2], new_id[RENAME ? kStep : 1];  // ids below kStep; half of them at most move
+  const int tid = threadIdx.x, lane = tid & 63;
+  int refs[kPerThread];
+  Pages hole = pass_at(0, p.n_pages), top = hole;
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u)
+    if (u < top.chunks) refs[u] = top.page(u) < p.n_pages ? p.page_refs[top.page(u)] : 0;
+  int count = 0, used, tops;
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u) {
+    top.bits[u] = u < top.chunks ? __ballot(refs[u] > 0) : 0;
+    hole.bits[u] = u < top.chunks ? ~top.bits[u] : 0;
+    count += __popcll(top.bits[u]);
+  }
+  waves_exclusive(count, sums, &used);
+  keep_below(hole, used);
+  const int holes = each_page(hole, 0, sums, [&](int k, int page) {
+    if (k < p.max_moves) {
+      dst_of[k] = (uint16_t)page;
+      p.move_dst[k] = page;
+    }
+  });
+  const int moves = holes < p.max_moves ? holes : p.max_moves;
+  for (int i = moves + tid; i < p.max_moves; i += kPlanThreads) p.move_src[i] = p.move_dst[i] = -1;
+  Pages below = top;
+  keep_below(below, used);
+  count = 0;
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u) {
+    top.bits[u] &= ~below.bits[u];
+    count += __popcll(top.bits[u]);
+  }
+  const uint64_t lower = lanes_below(lane);
+  int k = holes - 1 - waves_exclusive(count, sums, &tops);  // rank from the top  (the barrier also covers dst_of)
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u) {
+    if (u >= top.chunks) continue;
+    const int page = top.page(u);
+    int to = page;
+    if (top.bits[u] != 0) {
+      const int mine = k - __popcll(top.bits[u] & lower);
+      if ((top.bits[u] >> lane & 1) && mine < moves) {
+        to = dst_of[mine];
+        p.move_src[mine] = page;
+        p.page_refs[to] = refs[u];
+        p.page_refs[page] = 0;
+      }
+      k -= __popcll(top.bits[u]);
+    }
+    if (page < p.n_pages) p.page_map[page] = to;
+    if constexpr (RENAME) new_id[page] = (uint16_t)to;
+  }
+  if constexpr (RENAME) {
+    __syncthreads();
+    for (int e = tid; e < p.n_seqs * p.max_pages; e += kPlanThreads) {
+      const int id = p.block_table[e];
+      if (!maps(id, p.n_pages)) continue;
+      const int to = new_id[id];
+      if (to != id) p.block_table[e] = to;
+    }
+  }
+}
+
 __global__ __launch_bounds__(256) void rename_pages_kernel(int* block_table, size_t entries, const int* __restrict__ page_map, int n_pages) {
   const size_t e = (size_t)blockIdx.x * 256 + threadIdx.x;
   if (e >= entries) return;
@@ -303,16 +388,18 @@ __global__ __launch_bounds__(256) void rename_pages_kernel(int* block_table, siz
 }
 
 // ------------------------------------------------------------------------------------------------ reserve
+constexpr int kRowDepth = 5;  // loads in flight per lane: 80 entries of a row
+
 // Sixteen lanes: the row's unmapped entries below n_e take the pages of rank `rank` and on.  (Every lane of a wave calls it.)
 __device__ __forceinline__ void reserve_row(const ReserveParams& p, int s, int n_e, int rank, const int* pages) {
   const int lane = threadIdx.x & 63, l16 = lane & 15;
   int* row = p.block_table + (size_t)s * p.max_pages;
-  for (int e0 = 0; __any(e0 < n_e); e0 += 64) {
-    int id[4];
+  for (int e0 = 0; __any(e0 < n_e); e0 += 16 * kRowDepth) {
+    int id[kRowDepth];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) id[u] = e0 + 16 * u + l16 < n_e ? row[e0 + 16 * u + l16] : 0;
+    for (int u = 0; u < kRowDepth; ++u) id[u] = e0 + 16 * u + l16 < n_e ? row[e0 + 16 * u + l16] : 0;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < kRowDepth; ++u) {
       const bool missing = e0 + 16 * u + l16 < n_e && !maps(id[u], p.n_pages);
       const uint32_t who = (uint32_t)(__ballot(missing) >> (lane & 48)) & 0xffffu;
       if (missing) {
@@ -333,7 +420,7 @@ __global__ __launch_bounds__(kPlanThreads) void reserve_plan_kernel(ReserveParam
   int* owner = SMALL ? owner_lds : p.owner;
   int* pages = SMALL ? pages_lds : p.pages;
   const int tid = threadIdx.x;
-  const uint32_t first_mask = first_free_mask(p.page_refs, p.n_pages);
+  const Pages first_pass = free_pages(p.page_refs, 0, p.n_pages);
   for (int s = tid; s < p.n_seqs; s += kPlanThreads) put<SMALL>(owner + s, INT_MAX);
   const long most = (long)p.max_pages * kPage;
   auto named = [&](int i, int& s, int& len) {
@@ -354,8 +441,13 @@ __global__ __launch_bounds__(kPlanThreads) void reserve_plan_kernel(ReserveParam
     const int n_e = mine ? (len + kPage - 1) / kPage : 0;
     const int* row = p.block_table + (size_t)(mine ? s : 0) * p.max_pages;
     int missing = 0;
-#pragma unroll 4
-    for (int e = tid & 15; e < n_e; e += 16) missing += maps(row[e], p.n_pages) ? 0 : 1;
+    for (int e0 = tid & 15; e0 < n_e; e0 += 16 * kRowDepth) {
+      int id[kRowDepth];
+#pragma unroll
+      for (int u = 0; u < kRowDepth; ++u) id[u] = e0 + 16 * u < n_e ? row[e0 + 16 * u] : 0;  // (0 is a page)
+#pragma unroll
+      for (int u = 0; u < kRowDepth; ++u) missing += maps(id[u], p.n_pages) ? 0 : 1;
+    }
 #pragma unroll
     for (int step = 1; step < 16; step <<= 1) missing += __shfl_xor(missing, step, 16);
     if (mine && (tid & 15) == 0) put<SMALL>(first_of(i, s), missing);
@@ -374,7 +466,7 @@ __global__ __launch_bounds__(kPlanThreads) void reserve_plan_kernel(ReserveParam
     if (i < p.n) p.status[i] = !ok ? LORC_PAGES_REFUSED : missing;  // (the count, until it is known whether they are there)
   }
   plan_barrier();
-  const int found = each_free(p.page_refs, p.n_pages, first_mask, asked, sums, [&](int k, int page) { pages[k] = page; });
+  const int found = each_free(p.page_refs, p.n_pages, first_pass, asked, sums, [&](int k, int page) { pages[k] = page; });
   for (int i = tid; i < p.n; i += kPlanThreads) {
     int s, len;
     const bool ok = named(i, s, len) && get<SMALL>(owner + s) == i;
@@ -412,22 +504,33 @@ int launch_copy_pages(void* pool, size_t page_bytes, int n_pages, const int32_t*
                        n_pages, src, dst, (int)pieces);
 }
 
+// Waves of a row, 64 entries each: a wave that walks a row waits for memory at every step (256 forks of rows of 129 entries: 4.9 -> 3.8 us).
+static int waves_per_row(int n, int max_pages) {
+  const int want = (max_pages + 63) / 64, most = (1 << 30) / n;
+  return want < most ? want : most;
+}
+
 int launch_fork(const ForkParams& p, hipStream_t s) {
   const bool small = p.n <= kSmallList && p.n_seqs <= kSmallRows, rows = small && (long)p.n * p.max_pages <= kSmallTable;
   if (int rc = launch_kernel(rows ? fork_plan_kernel<true, true> : small ? fork_plan_kernel<true, false> : fork_plan_kernel<false, false>, dim3(1),
                              dim3(kPlanThreads), 0, s, p))
     return rc;
-  return rows ? LORC_OK : launch_kernel(fork_rows_kernel, dim3((p.n + 3) / 4), dim3(256), 0, s, p);
+  if (rows) return LORC_OK;
+  const int waves = waves_per_row(p.n, p.max_pages);
+  return launch_kernel(fork_rows_kernel, dim3((p.n * waves + 3) / 4), dim3(256), 0, s, p, waves);
 }
 
 int launch_free(int32_t* block_table, int n_seqs, int max_pages, int32_t* page_refs, int n_pages, const int32_t* seqs, int n, hipStream_t s) {
-  return launch_kernel(free_rows_kernel, dim3((n + 3) / 4), dim3(256), 0, s, block_table, n_seqs, max_pages, page_refs, n_pages, seqs, n);
+  const int waves = waves_per_row(n, max_pages);
+  return launch_kernel(free_rows_kernel, dim3((n * waves + 3) / 4), dim3(256), 0, s, block_table, n_seqs, max_pages, page_refs, n_pages, seqs, n, waves);
 }
 
 int launch_compact(const CompactParams& p, hipStream_t s) {
   const size_t entries = (size_t)p.n_seqs * p.max_pages;
-  const bool rename = entries <= kSmallTable;
-  if (int rc = launch_kernel(rename ? compact_plan_kernel<true> : compact_plan_kernel<false>, dim3(1), dim3(kPlanThreads), 0, s, p)) return rc;
+  const bool rename = entries <= kSmallTable, small = p.n_pages <= kStep;
+  if (int rc = launch_kernel(small ? (rename ? compact_small_kernel<true> : compact_small_kernel<false>)
+                                   : rename ? compact_plan_kernel<true> : compact_plan_kernel<false>, dim3(1), dim3(kPlanThreads), 0, s, p))
+    return rc;
   if (rename) return LORC_OK;
   return launch_kernel(rename_pages_kernel, dim3((uint32_t)((entries + 255) / 256)), dim3(256), 0, s, p.block_table, entries, p.page_map, p.n_pages);
 }
