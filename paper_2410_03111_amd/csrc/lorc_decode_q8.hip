@@ -7,6 +7,8 @@
 // scales are, the running reference of the softmax is M = max_t (s_t + k_t) instead of max_t s_t: the largest P' is then one, and
 // the sum of the weights is taken relative to the same M, l = sum 2^(s_t - M), in fp32.  (k_t counts as at least kLeastExp in M, which
 // bounds l; values below 448 x 2^kLeastExp are far below what the fp16 partials hold.)
+#include <climits>
+
 #include "lorc_device.h"
 #include "lorc_kernels.h"
 #include "lorc_q8.h"
@@ -390,6 +392,9 @@ bool q8_shape_ok(const lorc_layer_desc& d, Q8Form form, int max_ctx) {
   return max_ctx <= (1 << 30) && (max_ctx + kPage - 1) / kPage <= 512 * q8_walk(d, form).most;
 }
 
+// Splits: the workgroups run in rounds of what the device holds, a round lasts as long as its pages and the set-up of a workgroup,
+// which costs about two pages.  (One workgroup too many is a whole round.)
+constexpr long kQ8Rounds = 6, kQ8Setup = 2;
 DecodePlan make_q8_plan(const lorc_layer_desc& d, Q8Form form, int b, int max_ctx, int n_cus, int max_splits) {
   DecodePlan pl{};
   if (!q8_shape_ok(d, form, max_ctx)) return pl;
@@ -399,8 +404,17 @@ DecodePlan make_q8_plan(const lorc_layer_desc& d, Q8Form form, int b, int max_ct
   const auto [units, per_cu, most, kernel] = q8_walk(d, form);
   pl.stationary = kernel;
   const long least = (n_tiles + most - 1) / most;
-  long ns = (per_cu * (n_cus > 0 ? n_cus : 256) + b * units - 1) / (b * units);
-  if (ns > 64) ns = 64;
+  const long slots = per_cu * (n_cus > 0 ? n_cus : 256), first = (b * units + slots - 1) / slots;
+  long ns = 1, best = LONG_MAX;
+  for (long rounds = first; rounds < first + kQ8Rounds; ++rounds) {
+    const long most_here = rounds * slots / (b * units);
+    const long here = most_here > 64 ? 64 : most_here > n_tiles ? n_tiles : most_here;
+    const long cost = rounds * ((n_tiles + here - 1) / here + kQ8Setup);
+    if (cost < best) {
+      best = cost;
+      ns = here;
+    }
+  }
   if (ns > max_splits) ns = max_splits;
   if (ns < least) ns = least;
   if (ns > n_tiles) ns = n_tiles;
