@@ -210,9 +210,10 @@ __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeP
   };
   const uint32_t* q_src = qrot + (size_t)(kvh * gp + (l32 < gp && kvh * gp + l32 < n_heads ? l32 : 0)) * kStatQPitch + 16 * wq + 4 * hf;
   float* s_dst = sp + (size_t)(w * 16 + 4 * hf) * T + l32;
-  auto score = [&](f32x16& sa, const f16x8 (&kf)[2], auto part_c) {
+  auto query_operand = [&](auto part_c) { return *reinterpret_cast<const u32x4*>(q_src + 8 * decltype(part_c)::value); };
+  auto score = [&](f32x16& sa, const f16x8 (&kf)[2], const u32x4& q, auto part_c) {
     constexpr int part = decltype(part_c)::value;
-    sa = mfma32_f16(__builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4*>(q_src + 8 * part)), kf[part], part ? sa : zero16);
+    sa = mfma32_f16(__builtin_bit_cast(f16x8, q), kf[part], part ? sa : zero16);
   };
   auto score_store = [&](const f32x16& sa) {  // rows 8 (j / 4) + 4 hf + j % 4 (rows past the last head: filed, not read)
 #pragma unroll
@@ -319,6 +320,7 @@ __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeP
     PV pv[2];
     f32x4s al;
     i32x8 c[2];
+    u32x4 qf[2];
     c[0] = k_operand(buf, I0{});
     const int k_scale[2] = {k_scales(t, 0), k_scales(t, 4)};
     prev_acc = acc;
@@ -338,15 +340,17 @@ __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeP
       });
       // -- the previous half page: rotation and scores
       static_for<4>([&](auto i_c) {
-        if constexpr (x == at(decltype(i_c)::value)) rotate(kf, i_c);
+        if constexpr (x == at(2 * decltype(i_c)::value)) rotate(kf, i_c);
       });
-      if constexpr (x == at(4)) score(sa, kf, I0{});
-      if constexpr (x == at(5)) score(sa, kf, I1{});
-      if constexpr (x == at(7)) score_store(sa);
-      if constexpr (x == at(8)) lds_barrier();  // its scores are complete
+      if constexpr (x == at(0)) qf[0] = query_operand(I0{});
+      if constexpr (x == at(2)) qf[1] = query_operand(I1{});
+      if constexpr (x == at(4)) score(sa, kf, qf[0], I0{});
+      if constexpr (x == at(7)) score(sa, kf, qf[1], I1{});
+      if constexpr (x == at(9)) score_store(sa);
+      if constexpr (x == at(10)) lds_barrier();  // its scores are complete
       // -- its softmax, a pair of heads after the other
       static_for<PPH>([&](auto h_c) {
-        constexpr int h = decltype(h_c)::value, x0 = 8 + 4 * h;
+        constexpr int h = decltype(h_c)::value, x0 = 10 + 4 * h;
         if constexpr (x == at(x0)) softmax_load(sm, h, t + 1);  // (its buffers are those of the parity of t + 1)
         if constexpr (x == at(x0 + 1)) softmax_max(sm, valid_prev);
         if constexpr (x == at(x0 + 2)) softmax_rows(sm);
@@ -354,16 +358,16 @@ __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeP
         if constexpr (x == at(x0 + 3)) softmax_store(sm, h);
       });
       // -- this half page's queries
-      if constexpr (x == at(12)) qr.turns = (double)(q_pos - pos0) * turns_tab[lane];
-      if constexpr (x == at(13)) query_angle(qr);
-      if constexpr (x == at(15)) query_store(qr);
-      if constexpr (x == at(16)) lds_barrier();  // weights and queries are complete
+      if constexpr (x == at(11)) qr.turns = (double)(q_pos - pos0) * turns_tab[lane];
+      if constexpr (x == at(12)) query_angle(qr);
+      if constexpr (x == at(14)) query_store(qr);
+      if constexpr (x == at(18)) lds_barrier();  // weights and queries are complete
       // -- P' codes of the previous half page, a block's operands ahead
-      if constexpr (x == at(16)) al = *reinterpret_cast<const f32x4s*>(alpha + 4 * kg);
-      if constexpr (x == at(16)) pv_load(pv[0], prev, 0, T, false);
+      if constexpr (x == at(18)) al = *reinterpret_cast<const f32x4s*>(alpha + 4 * kg);
+      if constexpr (x == at(18)) pv_load(pv[0], prev, 0, T, false);
       static_for<VB>([&](auto i_c) {
         constexpr int i = decltype(i_c)::value;
-        if constexpr (x == at(17 + i * 15 / VB)) {
+        if constexpr (x == at(19 + i * 13 / VB)) {
           if constexpr (i + 1 < VB) pv_load(pv[(i + 1) % 2], prev, i + 1, T, false);
           pv_mul(pv[i % 2], al, i_c);
         }
@@ -380,8 +384,8 @@ __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeP
     f32x16 sa;
     prev_acc = acc;
     static_for<4>([&](auto i_c) { rotate(kf, i_c); });
-    score(sa, kf, I0{});
-    score(sa, kf, I1{});
+    score(sa, kf, query_operand(I0{}), I0{});
+    score(sa, kf, query_operand(I1{}), I1{});
     score_store(sa);
     dma_barrier<0>();  // scores complete; its V and scales have landed
 #pragma unroll
