@@ -24,6 +24,9 @@ constexpr double kTurns = 0.15915494309189533576888;  // 1 / 2 pi
 // One workgroup of four waves per (sequence, context split, block of 32 query heads), 32 positions at a time.  The step's K codes are
 // widened once into LDS (bf16, operand order), wave w takes every fourth k-step of the scores, partial scores meet in LDS, eight lanes
 // per head take the softmax, and wave w owns every fourth block of 32 value latents, whose codes it loads itself, ahead of the scores.
+// Bound by the chain of four phases and their barriers, one workgroup per compute unit: rank 1024, 16 x 4096 positions 118 us with the merge
+// (bf16 pages, twice the bytes: 90).  The kernel for ranks up to 512 keeps two buffers of pages in LDS, which do not fit here; where both
+// can serve (16 x 8192, rank 512) it takes 40 us and a form like this one 172.
 __global__ __launch_bounds__(256, 1) void decode_q8_kernel(DecodeParams p) {
   constexpr int T = 32, NBW = 8;
   extern __shared__ __align__(16) unsigned char smem[];
@@ -182,6 +185,7 @@ __global__ __launch_bounds__(256, 1) void decode_q8_kernel(DecodeParams p) {
 // coordinates, so that row r of block b is position (coordinate) 2 r + b of the step and a lane's eight scores are those of eight
 // consecutive positions, which is what it holds of V.  Keys take the angles of their offset in the step, constants in fp16 like the
 // keys themselves; the base goes to the queries (one frequency per lane, handed round through LDS).
+// Bound by the page stream: 16 x 4096 positions of 2 KiB in 29.6 us, 4.5 TB/s (bf16 pages: 46 us), the merge 4.5 more.
 template <bool BOTH>
 __global__ __launch_bounds__(256, 2) void decode_plain_q8_kernel(DecodeParams p) {
   constexpr int HD = 128, HALF = 64, T = 32;
@@ -368,7 +372,9 @@ size_t q8_lds_bytes(const lorc_layer_desc& d) {
 }  // namespace
 
 namespace {
-// Which kernel, and how it divides a sequence: workgroups per (sequence, split), those that share a compute unit, the pages that a split
+// Which kernel, and how it divides a sequence.  Rotary: stationary where its registers hold the factor, wide for the rest (16 x 4096 positions
+// on either: 32/8 heads rank 512 77 / 122 us, rank 128 43 / 76, 16/16 heads rank 192 78 / 209).  Absorbed: the two page buffers decide.
+// Walk: workgroups per (sequence, split), those that share a compute unit, the pages that a split
 // walks at most (their ids live in LDS).
 struct Q8Walk {
   long units, per_cu, most;
@@ -393,7 +399,9 @@ bool q8_shape_ok(const lorc_layer_desc& d, Q8Form form, int max_ctx) {
 }
 
 // Splits: the workgroups run in rounds of what the device holds, a round lasts as long as its pages and the set-up of a workgroup,
-// which costs about two pages.  (One workgroup too many is a whole round.)
+// which costs about two pages.  One workgroup too many is a whole round: against the fewest splits that give every compute unit one, rank
+// 512, 12 x 4096 positions 95 -> 64 us, 24 x 4096 161 -> 121, 40 KV heads 8 x 2000 125 -> 98, absorbed 24 x 4096 54 -> 41.  (Lengths are on the
+// device: sequences count as max_ctx here.)
 constexpr long kQ8Rounds = 6, kQ8Setup = 2;
 DecodePlan make_q8_plan(const lorc_layer_desc& d, Q8Form form, int b, int max_ctx, int n_cus, int max_splits) {
   DecodePlan pl{};

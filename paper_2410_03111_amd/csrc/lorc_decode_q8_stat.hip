@@ -14,6 +14,11 @@
 //   its P' codes_V;  this tile's first block: rotation, scores.
 // Keys are rotated by their offset in the tile (fp16 constants), queries by the distance to its first position.  Weights carry the
 // values' scales: see lorc_decode_q8.hip.
+//
+// Bound by the matrix cores beside the vector instructions of rotation, softmax and conversion: 32/8 heads, rank 512, 16 x 4096 positions
+// 70 us (68.7 GFLOP of rebuild, taken twice), matrix cores busy 61 %; a longer context adds 1147 TFLOP/s, a bf16 product of 8192^3 on the
+// same card 1200.  bf16 pages: 76 us.  64/8 heads, 64 x 8192: 527 us (579).  Two waves per SIMD, not one: the waits of one are the
+// products of the other (the wide form takes 122 us for the first shape).
 #include "lorc_device.h"
 #include "lorc_kernels.h"
 #include "lorc_q8.h"
@@ -143,7 +148,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
       const int b = w + NW * i, pb = b >= k_rows ? 1 : 0, c = b - pb * k_rows;
       if (b < k_blocks) dma_1k(r, uniform_u32(k_lds + (uint32_t)(buf * NS * 4096 + pb * NS * 2048 + c * 1024)), lane16, uniform_u32((uint32_t)b * 1024u));
     }
-    if (w == 0) dma_256(r, uniform_u32(s_lds + (uint32_t)(buf * kQ8ScaleBytes)), lane4, uniform_u32((uint32_t)(64 * (r_k + r_v))));
+    if (w == 0) dma_256(r, uniform_u32(s_lds + (uint32_t)(buf * kQ8ScaleBytes)), lane4, uniform_u32((uint32_t)(64 * (r_k + r_v))));  // (begins in the page; lanes behind its end read zeros)
   };
   auto copy_v = [&](int id, int buf) {
     const u32x4 r = rsrc_of(id);
@@ -421,7 +426,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
     score(sa, kf, I0{});
     score(sa, kf, I1{});
     score_store(sa, I1{});
-    lds_barrier();
+    dma_barrier<0>();  // scores complete; its V codes and scales have landed
 #pragma unroll
     for (int h = 0; h < PPH; ++h) {
       softmax_load(sm[h], h, prev);
@@ -430,7 +435,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
       softmax_weight(sm[h], h);
       softmax_store(sm[h], h);
     }
-    dma_barrier<0>();  // weights visible; the V codes have landed
+    lds_barrier();  // weights visible
     pv_prep(pv);
     pv_load(pv, prev, 0, valid_prev, valid_prev < T);
     pv_mul(pv, I0{});

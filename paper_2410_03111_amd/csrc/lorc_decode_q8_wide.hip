@@ -3,9 +3,13 @@
 //
 // The same products (the pages' codes against B_k as pairs of e4m3 codes, held in registers), with one wave per SIMD: four waves of up
 // to 512 registers own one KV head of head_dim 128 (or two of 64) of one (sequence, context split) and up to sixteen query heads; a wave
-// holds 32 columns, 16 registers per 64 latent indices (256 at rank 1024).  Half pages of 32 positions keep K and V in two buffers each within the LDS.  A
-// product takes 64 cycles of the matrix core and the next one of the wave waits for it, so everything else is laid between the
-// products of the next half page's rebuild: rotation and scores;  barrier;  softmax, queries;  barrier;  P' codes_V.
+// holds 32 columns, 16 registers per 64 latent indices (256 at rank 1024).  Half pages of 32 positions keep K and V in two buffers each
+// within the LDS.  A product takes 64 cycles of the matrix core and the next one of the wave waits for it, so everything else is laid
+// between the products of the next half page's rebuild: rotation and scores;  barrier;  softmax, queries;  barrier;  P' codes_V.
+//
+// Bound by what a single wave cannot hide (rank 768: matrix cores busy 36 %, vector instructions 29 %, waits 22 %).  32/8 heads, 16 x 4096
+// positions, with the merge (bf16 pages in brackets): rank 576 120 us (90), 768 126 to 139 (110 to 127), 1024 157 (192); 32/2 heads rank 256
+// 39 (88); 24/8 heads of 64, rank 256 51 (44), rank 512 62 (68).
 #include "lorc_device.h"
 #include "lorc_kernels.h"
 #include "lorc_q8.h"
@@ -148,7 +152,9 @@ __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeP
   const uint32_t lane4 = 4u * (uint32_t)lane, lane16 = 16u * (uint32_t)lane;
   constexpr int NKC = (2 * NS + NW - 1) / NW, NVC = VB;  // copies per wave, and two of scale bytes each
   auto copy_scales = [&](const u32x4& r, int part, int buf, int i) {  // part: 0 K, 1 V
-    dma_256(r, uniform_u32(s_lds + (uint32_t)((2 * part + buf) * kWideScales + 256 * i)), lane4, uniform_u32((uint32_t)(64 * (r_k + r_v + (part ? gk : 0)) + 256 * i)));
+    // (the place in the lane offset: of few groups the second block begins behind the page, where a scalar offset is not checked)
+    const uint32_t from = 64u * (uint32_t)(r_k + r_v + (part ? gk : 0)) + 256u * (uint32_t)i;
+    dma_256(r, uniform_u32(s_lds + (uint32_t)((2 * part + buf) * kWideScales + 256 * i)), lane4 + from, 0u);
   };
   auto copy_k = [&](const u32x4& r, int t, int i) {
     const int buf = t & 1, sb = t & 1;

@@ -315,6 +315,24 @@ def test_replays_from_a_graph_on_another_stream(name):
         assert torch.equal(got, out) and bool(torch.isfinite(got).all()), rep
 
 
+@pytest.mark.parametrize("name", FORMS)
+def test_short_sequences_whose_pages_come_from_memory(name):
+    """The one page of a sequence is asked for and used within a few hundred cycles: nothing may be read before it has landed.  Between the
+    calls the caches are filled with something else, and LDS with the scales of much larger values."""
+    import torch
+    c = Cache8(ctx=[1 + 3 * s % 64 for s in range(96)], seed=19, **FORMS[name])
+    other = Cache8(ctx=[200, 64, 130], seed=20, amp_v=2.0 ** 40, **FORMS[name])
+    other.block_table, other.ctx = other.block_table.repeat(32, 1), other.ctx * 32
+    other.dq = other.dq.repeat(32, 1, 1)
+    want = c.call()
+    c.check(got=want)
+    large = torch.empty(3 << 28, dtype=torch.uint8, device="cuda")
+    for rep in range(12):
+        other.call()
+        large.fill_(rep)
+        assert torch.equal(c.call(), want), rep
+
+
 @pytest.mark.parametrize("name", ["plain", "absorbed", "rotary"])
 def test_rows_of_the_table_behind_the_batch_and_refused_arguments(name):
     import torch
