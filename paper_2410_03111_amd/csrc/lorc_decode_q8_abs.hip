@@ -112,7 +112,8 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_absorbed_kernel(Dec
       const int pb = b >= k_rows ? 1 : 0, c = b - pb * k_rows;
       dma_1k(r, uniform_u32(k_lds + (uint32_t)(buf * KB + pb * (KB / 2) + c * 1024)), lane16, uniform_u32((uint32_t)b * 1024u));
     }
-    dma_256(r, uniform_u32(s_lds + (uint32_t)(buf * 512)), lane16 >> 2, uniform_u32((uint32_t)(64 * (r_k + r_v))));  // (begins in the page; lanes behind its end read zeros)
+    // (both begin in the page, lanes behind its end read zeros)
+    dma_256(r, uniform_u32(s_lds + (uint32_t)(buf * 512)), lane16 >> 2, uniform_u32((uint32_t)(64 * (r_k + r_v))));
     dma_256(r, uniform_u32(s_lds + (uint32_t)(buf * 512 + 256)), lane16 >> 2, uniform_u32((uint32_t)(64 * (r_k + r_v + gk))));
   };
   auto copy_v = [&](int id, int buf) {

@@ -114,7 +114,8 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
         const u32x4 b = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at + 1024u, 0, 0));
         fac[s][u] = i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
       }
-    const u32x2 sc = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, real ? (uint32_t)steps * n * 128u + (uint32_t)(block * 32 + l32) * (uint32_t)kCodedMaxSteps : 0x7fff0000u, 0, 0));
+    const u32x2 sc = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(
+        r, real ? (uint32_t)steps * n * 128u + (uint32_t)(block * 32 + l32) * (uint32_t)kCodedMaxSteps : 0x7fff0000u, 0, 0));
     fac_scale[0] = (int)sc[0];
     fac_scale[1] = (int)sc[1];
   }
@@ -148,7 +149,8 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
       const int b = w + NW * i, pb = b >= k_rows ? 1 : 0, c = b - pb * k_rows;
       if (b < k_blocks) dma_1k(r, uniform_u32(k_lds + (uint32_t)(buf * NS * 4096 + pb * NS * 2048 + c * 1024)), lane16, uniform_u32((uint32_t)b * 1024u));
     }
-    if (w == 0) dma_256(r, uniform_u32(s_lds + (uint32_t)(buf * kQ8ScaleBytes)), lane4, uniform_u32((uint32_t)(64 * (r_k + r_v))));  // (begins in the page; lanes behind its end read zeros)
+    // (the scales of K: the copy begins in the page, lanes behind its end read zeros)
+    if (w == 0) dma_256(r, uniform_u32(s_lds + (uint32_t)(buf * kQ8ScaleBytes)), lane4, uniform_u32((uint32_t)(64 * (r_k + r_v))));
   };
   auto copy_v = [&](int id, int buf) {
     const u32x4 r = rsrc_of(id);
