@@ -289,7 +289,7 @@ int lorc_prefill_attention_plain(const lorc_layer_desc* desc, const void* q, con
  *   page_refs   [n_pages] int32: how many entries map the page; pages whose count is not positive are free
  * One table and one count array may serve the pools of all layers: the calls that change them return which pages to copy, and
  * lorc_copy_pages is called once per pool.  Results do not depend on timing: pages are given out by rank.  A call reads its
- * lists when it runs on the stream; a list of 0 entries is LORC_OK.  Tables, counts and lists have up to 2^30 entries.  status[i] (one per list entry) is one of: */
+ * lists when it runs on the stream; a list of 0 entries is LORC_OK, its pointers may be NULL.  Tables, counts and lists have up to 2^30 entries.  status[i] (one per list entry) is one of: */
 #define LORC_PAGES_OK 0
 #define LORC_PAGES_REFUSED 1 /* an index or length out of range, a row that the call cannot take (see there): nothing changed for it */
 #define LORC_PAGES_SHORT 2   /* not enough free pages: nothing changed for it                                                       */

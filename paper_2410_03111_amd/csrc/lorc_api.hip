@@ -397,6 +397,7 @@ int lorc_prefill_attention_plain(const lorc_layer_desc* desc, const void* q, con
 namespace {
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 constexpr int kMostEntries = 1 << 30;  // of tables, counts and lists: what a plan adds up and steps over stays below 2^31
+// (asked before a list's pointers are: a list of no entries needs none, and an empty tensor has none)
 bool list_ok(int32_t n) { return n >= 0 && n <= kMostEntries; }
 int table_args(const void* block_table, int32_t n_seqs, int32_t max_pages, const void* page_refs, int32_t n_pages) {
   if (!block_table || !page_refs || n_seqs <= 0 || max_pages <= 0 || n_pages <= 0) return LORC_EINVAL;
@@ -411,8 +412,9 @@ size_t lorc_pages_workspace_bytes(int32_t n_seqs, int32_t n_pages) {
 }
 
 int lorc_copy_pages(void* pool, size_t page_bytes, int32_t n_pages, const int32_t* src, const int32_t* dst, int32_t count, void* stream) {
-  if (!pool || !src || !dst || n_pages <= 0 || count < 0 || page_bytes == 0 || (page_bytes & 15) || !aligned16(pool)) return LORC_EINVAL;
+  if (!pool || n_pages <= 0 || !list_ok(count) || page_bytes == 0 || (page_bytes & 15) || !aligned16(pool)) return LORC_EINVAL;
   if (count == 0) return LORC_OK;
+  if (!src || !dst) return LORC_EINVAL;
   return launch_copy_pages(pool, page_bytes, n_pages, src, dst, count, static_cast<hipStream_t>(stream));
 }
 
@@ -420,10 +422,11 @@ int lorc_fork_sequences(int32_t* block_table, int32_t n_seqs, int32_t max_pages,
                         const int32_t* parents, const int32_t* children, const int32_t* lens, int32_t n, int32_t* copy_src,
                         int32_t* copy_dst, int32_t* status, void* workspace, size_t workspace_bytes, void* stream) {
   if (int rc = table_args(block_table, n_seqs, max_pages, page_refs, n_pages)) return rc;
-  if (!parents || !children || !lens || !copy_src || !copy_dst || !status || !workspace || !list_ok(n)) return LORC_EINVAL;
+  if (!workspace || !list_ok(n)) return LORC_EINVAL;
   if (reinterpret_cast<uintptr_t>(workspace) & 255) return LORC_EINVAL;
   if (workspace_bytes < lorc_pages_workspace_bytes(n_seqs, n_pages)) return LORC_EWORKSPACE;
   if (n == 0) return LORC_OK;
+  if (!parents || !children || !lens || !copy_src || !copy_dst || !status) return LORC_EINVAL;
   ForkParams p;
   p.block_table = block_table;
   p.page_refs = page_refs;
@@ -445,8 +448,9 @@ int lorc_fork_sequences(int32_t* block_table, int32_t n_seqs, int32_t max_pages,
 int lorc_free_sequences(int32_t* block_table, int32_t n_seqs, int32_t max_pages, int32_t* page_refs, int32_t n_pages,
                         const int32_t* seqs, int32_t n, void* stream) {
   if (int rc = table_args(block_table, n_seqs, max_pages, page_refs, n_pages)) return rc;
-  if (!seqs || !list_ok(n)) return LORC_EINVAL;
+  if (!list_ok(n)) return LORC_EINVAL;
   if (n == 0) return LORC_OK;
+  if (!seqs) return LORC_EINVAL;
   return launch_free(block_table, n_seqs, max_pages, page_refs, n_pages, seqs, n, static_cast<hipStream_t>(stream));
 }
 
@@ -471,10 +475,11 @@ int lorc_reserve_pages(int32_t* block_table, int32_t n_seqs, int32_t max_pages, 
                        const int32_t* seqs, const int32_t* lens, int32_t n, int32_t* status, void* workspace,
                        size_t workspace_bytes, void* stream) {
   if (int rc = table_args(block_table, n_seqs, max_pages, page_refs, n_pages)) return rc;
-  if (!seqs || !lens || !status || !workspace || !list_ok(n)) return LORC_EINVAL;
+  if (!workspace || !list_ok(n)) return LORC_EINVAL;
   if (reinterpret_cast<uintptr_t>(workspace) & 255) return LORC_EINVAL;
   if (workspace_bytes < lorc_pages_workspace_bytes(n_seqs, n_pages)) return LORC_EWORKSPACE;
   if (n == 0) return LORC_OK;
+  if (!seqs || !lens || !status) return LORC_EINVAL;
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   ReserveParams p;
   p.block_table = block_table;
