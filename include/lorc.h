@@ -305,7 +305,8 @@ int lorc_copy_pages(void* pool, size_t page_bytes, int32_t n_pages, const int32_
 /* Row children[i] becomes a continuation of the first lens[i] positions of row parents[i], i < n: whole pages are shared, a last page
  * that is not full becomes a page of the child's own (the lowest free one), which has to be filled from the parent's:
  *   copy_src, copy_dst [n]  the pair to copy, -1 where there is none
- * Entries of the parent that map nothing stay unmapped in the child; the rest of the child's row maps nothing.
+ * Entries of the parent that map nothing stay unmapped in the child; the rest of the child's row maps nothing.  Pages that the child's row
+ * mapped behind its first entry lose a count, as by lorc_free_sequences (none of them is given out by the same call).
  * LORC_PAGES_REFUSED: a row outside the table, lens[i] outside [0, 64 max_pages], parents[i] = children[i], a child whose first entry
  * maps a page (free it first) or that an earlier pair names, a parent that any pair names as its child.  Pairs are served in order:
  * once free pages run out, the pairs that need one are LORC_PAGES_SHORT. */

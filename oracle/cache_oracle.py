@@ -45,6 +45,9 @@ class Pages:
                     continue
                 src[-1], dst[-1] = tail, free.pop(0)
             status.append(OK)
+            for e in range(len(self.table[c])):
+                if self.maps(before[c, e]):
+                    self.refs[before[c, e]] -= 1
             self.table[c] = -1
             for e in range(L // PAGE):
                 if self.maps(before[p, e]):

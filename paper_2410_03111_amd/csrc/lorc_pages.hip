@@ -168,12 +168,15 @@ __global__ __launch_bounds__(256) void copy_pages_kernel(unsigned char* pool, si
 }
 
 // ------------------------------------------------------------------------------------------------ fork
-// One wave, or `waves` of them: the child's row, and the counts of the pages that it shares.
+// One wave, or `waves` of them: the child's row, the counts of the pages that it shares, and of those that the row mapped before (behind a
+// first entry that maps nothing).  The plan gave out its pages before any row is changed: what a row releases is free for the next call.
 __device__ __forceinline__ void fork_row(const ForkParams& p, int parent, int child, int len, int fresh, int wave = 0, int waves = 1) {
   const int whole = len / kPage, *from = p.block_table + (size_t)parent * p.max_pages;
   int* to = p.block_table + (size_t)child * p.max_pages;
   for (int e = 64 * wave + (int)(threadIdx.x & 63); e < p.max_pages; e += 64 * waves) {
     int id = e < whole ? from[e] : e == whole ? fresh : -1;
+    const int old = to[e];
+    if (maps(old, p.n_pages)) atomicSub(p.page_refs + old, 1);
     if (!maps(id, p.n_pages)) id = -1;
     else if (e < whole) atomicAdd(p.page_refs + id, 1);
     else p.page_refs[id] = 1;
