@@ -25,7 +25,9 @@
  *     rebuilt keys or values exceed about 6e4 in magnitude give inf/NaN outputs; latents of the size that
  *     normalised hidden states produce (O(1) .. O(100)) are far inside the range.
  *   - Return value: LORC_OK (0) or a negative lorc_status; lorc_strerror() gives the text.  Shapes are
- *     validated on the host before anything is launched; LORC_EHIP is the status of this call's own launch.
+ *     validated on the host before anything is launched; LORC_EHIP is the status of this call's own launch,
+ *     LORC_EINVAL that of one which would need 2^32 work-items or more, what the hardware takes at once
+ *     (lists of pages and prompts that are quantised go out in as many launches as they need).
  *   - Query head h reads KV head h / G.  RoPE pairs coordinate i with i + d/2, theta_i = base^(-2i/d).
  *
  * Latent cache (device, caller-allocated):  a pool of pages, each holding LORC_PAGE_TOKENS = 64

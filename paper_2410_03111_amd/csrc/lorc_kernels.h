@@ -13,6 +13,21 @@
 
 namespace lorc {
 
+// A launch holds fewer than 2^32 work-items along a dimension.  The runtime takes a larger grid without an error and runs what is left of it
+// modulo 2^32, so that every launch is checked here; calls whose lists may need more go out in parts of launch_blocks().
+constexpr int launch_blocks(int threads) { return (int)(((uint64_t)1 << 32) / (uint64_t)threads) - 1; }
+// part(first, count) for [0, n) in parts of `most`, until one fails.
+template <typename F>
+inline int launch_parts(int n, int most, F part) {
+  if (most <= 0) return LORC_EINVAL;  // (one entry is more than a launch holds)
+  for (int first = 0; first < n;) {
+    const int count = n - first < most ? n - first : most;
+    if (int rc = part(first, count)) return rc;
+    first += count;
+  }
+  return LORC_OK;
+}
+
 // One kernel launch that reports its own status.  (hipGetLastError() after a <<<>>> launch would also return, and
 // clear, an error left behind by an unrelated earlier call of the process.)
 template <typename... KArgs, size_t... I>
@@ -24,6 +39,7 @@ inline hipError_t launch_kernel_impl(void (*kern)(KArgs...), dim3 grid, dim3 blo
 template <typename... KArgs, typename... Args>
 inline int launch_kernel(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t lds, hipStream_t s, Args&&... args) {
   static_assert(sizeof...(KArgs) == sizeof...(Args), "argument count of the kernel");
+  if (((uint64_t)grid.x * block.x | (uint64_t)grid.y * block.y | (uint64_t)grid.z * block.z) >> 32) return LORC_EINVAL;
   std::tuple<KArgs...> held(static_cast<KArgs>(std::forward<Args>(args))...);
   return launch_kernel_impl(kern, grid, block, lds, s, held, std::index_sequence_for<KArgs...>{}) == hipSuccess
              ? LORC_OK : LORC_EHIP;
@@ -135,6 +151,7 @@ struct QuantizeParams {
   unsigned char* dst;
   const int32_t *src_table, *dst_table, *pos_begin, *pos_end;
   int b, max_tokens, span;  // span: pages that max_tokens positions can touch
+  int first;                // workgroup of the call that this launch begins with
   int r_k, r_v, src_max_pages, src_pages, dst_max_pages, dst_pages;
 };
 

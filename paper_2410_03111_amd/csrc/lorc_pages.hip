@@ -507,9 +507,10 @@ __global__ __launch_bounds__(256) void reserve_rows_kernel(ReserveParams p) {
 // ------------------------------------------------------------------------------------------------ host
 int launch_copy_pages(void* pool, size_t page_bytes, int n_pages, const int32_t* src, const int32_t* dst, int count, hipStream_t s) {
   const size_t pieces = (page_bytes + kCopyBytes - 1) / kCopyBytes;
-  if (pieces * (size_t)count > 0x7fffffffu) return LORC_EINVAL;
-  return launch_kernel(copy_pages_kernel, dim3((uint32_t)(pieces * count)), dim3(256), 0, s, static_cast<unsigned char*>(pool), page_bytes,
-                       n_pages, src, dst, (int)pieces);
+  return launch_parts(count, (int)(launch_blocks(256) / pieces), [&](int first, int n) {
+    return launch_kernel(copy_pages_kernel, dim3((uint32_t)(pieces * n)), dim3(256), 0, s, static_cast<unsigned char*>(pool), page_bytes, n_pages,
+                         src + first, dst + first, (int)pieces);
+  });
 }
 
 // Waves of a row, 64 entries each: a wave that walks a row waits for memory at every step (256 forks of rows of 129 entries: 4.9 -> 3.8 us).
@@ -525,12 +526,24 @@ int launch_fork(const ForkParams& p, hipStream_t s) {
     return rc;
   if (rows) return LORC_OK;
   const int waves = waves_per_row(p.n, p.max_pages);
-  return launch_kernel(fork_rows_kernel, dim3((p.n * waves + 3) / 4), dim3(256), 0, s, p, waves);
+  return launch_parts(p.n, 4 * launch_blocks(256) / waves, [&](int first, int n) {
+    ForkParams part = p;
+    part.parents += first;
+    part.children += first;
+    part.lens += first;
+    part.status += first;
+    part.copy_dst += first;
+    part.n = n;
+    return launch_kernel(fork_rows_kernel, dim3((n * waves + 3) / 4), dim3(256), 0, s, part, waves);
+  });
 }
 
 int launch_free(int32_t* block_table, int n_seqs, int max_pages, int32_t* page_refs, int n_pages, const int32_t* seqs, int n, hipStream_t s) {
   const int waves = waves_per_row(n, max_pages);
-  return launch_kernel(free_rows_kernel, dim3((n * waves + 3) / 4), dim3(256), 0, s, block_table, n_seqs, max_pages, page_refs, n_pages, seqs, n, waves);
+  return launch_parts(n, 4 * launch_blocks(256) / waves, [&](int first, int here) {
+    return launch_kernel(free_rows_kernel, dim3((here * waves + 3) / 4), dim3(256), 0, s, block_table, n_seqs, max_pages, page_refs, n_pages, seqs + first,
+                         here, waves);
+  });
 }
 
 int launch_compact(const CompactParams& p, hipStream_t s) {
@@ -548,7 +561,15 @@ int launch_reserve(const ReserveParams& p, hipStream_t s) {
   const bool rows = p.n <= kSmallList && p.n_seqs <= kSmallRows && (long)p.n * p.max_pages <= kSmallTable;
   if (int rc = launch_kernel(rows ? reserve_plan_kernel<true> : reserve_plan_kernel<false>, dim3(1), dim3(kPlanThreads), 0, s, p))
     return rc;
-  return rows ? LORC_OK : launch_kernel(reserve_rows_kernel, dim3((p.n + 15) / 16), dim3(256), 0, s, p);
+  if (rows) return LORC_OK;
+  return launch_parts(p.n, 16 * launch_blocks(256), [&](int first, int n) {
+    ReserveParams part = p;
+    part.seqs += first;
+    part.lens += first;
+    part.status += first;
+    part.n = n;
+    return launch_kernel(reserve_rows_kernel, dim3((n + 15) / 16), dim3(256), 0, s, part);
+  });
 }
 
 }  // namespace lorc

@@ -33,7 +33,7 @@ __device__ __forceinline__ float elem(const u32x4& v, int e) { return __uint_as_
 __global__ __launch_bounds__(256) void quantize_latents_kernel(QuantizeParams p) {
   const int gk = q8_groups(p.r_k), gv = q8_groups(p.r_v), units = 2 * gk + 4 * gv, blocks = (units + 3) / 4;
   const int lane = threadIdx.x & 63, hf = lane >> 5, l32 = lane & 31;
-  int i = blockIdx.x;
+  int i = p.first + (int)blockIdx.x;
   const int unit = (i % blocks) * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   i /= blocks;
   const int seq = i / p.span, nth = i % p.span;
@@ -153,7 +153,11 @@ int launch_quantize(const QuantizeParams& p, hipStream_t s) {
   const int units = 2 * q8_groups(p.r_k) + 4 * q8_groups(p.r_v);
   const size_t blocks = (size_t)p.b * p.span * ((units + 3) / 4);
   if (blocks > 0x7fffffffu) return LORC_EINVAL;
-  return launch_kernel(quantize_latents_kernel, dim3((uint32_t)blocks), dim3(256), 0, s, p);
+  return launch_parts((int)blocks, launch_blocks(256), [&](int first, int count) {
+    QuantizeParams part = p;
+    part.first = first;
+    return launch_kernel(quantize_latents_kernel, dim3((uint32_t)count), dim3(256), 0, s, part);
+  });
 }
 
 }  // namespace lorc
