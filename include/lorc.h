@@ -363,6 +363,9 @@ int lorc_quantize_latents(const lorc_layer_desc* desc, const void* cache, const 
  * lorc_decode_attention_absorbed on the values that the pages stand for, with cache and n_pages those of the 8-bit pool.
  *   workspace   lorc_decode_quantized_workspace_bytes (lorc_decode_plain_..., lorc_decode_absorbed_...) bytes, 256-byte aligned, or as many as any call
  *               with at least this b and max_ctx asks for
+ * Value groups of one position share a softmax reference: in a group 2^-j of the position's largest, weights keep their bits to 2^(j - 29) of the
+ * largest weight and are zero below 2^(j - 40) (rotary and absorbed; an uncompressed layer's heads have a reference each).  The rotary form
+ * takes an entry of B_k within 2^-17 of the largest of its column and 64 latents, the absorbed one an entry of q_lat within as much of its 128.
  * rotary: ranks up to 1024, max_ctx up to 2^22;  uncompressed: head_dim 128, rank_k = rank_v = n, max_ctx up to 2^30;  absorbed: ranks up to 1024,
  * max_ctx up to 2^25;  64 query heads each;  otherwise the workspace size is 0 and the call LORC_EUNSUPPORTED. */
 size_t lorc_decode_quantized_workspace_bytes(const lorc_layer_desc* desc, int32_t b, int32_t max_ctx);

@@ -4,9 +4,13 @@
 // conversion of the codes (which takes a power of two for free).  A value's scale belongs to a position too, which is the
 // contraction index of P V: it goes into the weights, P'_t = p_t 2^(k_t), and the codes are multiplied as they are.
 // Weights and codes are fp16 there (a code has four significant bits, the weights keep eleven).  To keep P' in range whatever the
-// scales are, the running reference of the softmax is M = max_t (s_t + k_t) instead of max_t s_t: the largest P' is then one, and
-// the sum of the weights is taken relative to the same M, l = sum 2^(s_t - M), in fp32.  (k_t counts as at least kLeastExp in M, which
-// bounds l; values below 448 x 2^kLeastExp are far below what the fp16 partials hold.)
+// scales are, the running reference of the softmax is M = max_t (s_t + k_t) - kTopExp instead of max_t s_t: the largest P' is then 2^15, the
+// top of fp16, and the sum of the weights is taken relative to the same M, l = sum 2^(s_t - M), in fp32.  (k_t counts as at least kLeastExp in
+// M, which bounds l; values below 448 x 2^kLeastExp are far below what the fp16 partials hold.)
+// k_t is the largest over the groups of the position, as one reference serves all of them.  In a group that is 2^-j of the largest, a weight
+// that is 2^-i of the largest has P' = 2^(15 - i - j): all eleven bits to i + j = 29, none beyond 40.  (With the largest P' at one, it would be 14
+// and 25: groups that lie 2^16 apart and count alike in the output cost 2 to 3 % of it.)  An uncompressed layer's groups are its KV heads, which
+// have a reference each; there the largest P' is one.
 #include <climits>
 
 #include "lorc_device.h"
@@ -110,7 +114,7 @@ __global__ __launch_bounds__(256, 1) void decode_q8_kernel(DecodeParams p) {
           const uint32_t b = (ub[g] >> (8 * e)) & 255u;
           top = g < gv && b > top ? b : top;
         }
-        mx = fmaxf(mx, s[e] + ((float)top - 127.f));
+        mx = fmaxf(mx, s[e] + ((float)top - (127.f + kTopExp)));
       }
 #pragma unroll
       for (int step = 1; step < 8; step <<= 1) mx = fmaxf(mx, __shfl_xor(mx, step, 64));
@@ -127,7 +131,7 @@ __global__ __launch_bounds__(256, 1) void decode_q8_kernel(DecodeParams p) {
         for (int g = 0; g < 8; ++g)
           if (g < gv)
             pb[((size_t)(g * 2 + (pos >> 4)) * 64 + sh + 32 * ((pos & 15) >> 3)) * 8 + (pos & 7)] =
-                f16_bits(__builtin_amdgcn_ldexpf(pe, (int)((ub[g] >> (8 * e)) & 255u) - 127));
+                f16_bits(below_f16_max(__builtin_amdgcn_ldexpf(pe, (int)((ub[g] >> (8 * e)) & 255u) - 127)));
       }
     }
     __syncthreads();

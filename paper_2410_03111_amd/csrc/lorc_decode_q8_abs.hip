@@ -236,7 +236,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_absorbed_kernel(Dec
       s4 = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(qa[g][1], kb, s4, 0, 0, g, q_bytes, g, k_bytes);
     });
     // ---- softmax: row maxima of the wave's 16 positions, exchanged between the four position blocks
-    const float k_top = (float)top - 127.f;
+    const float k_top = (float)top - (127.f + kTopExp);
     float s[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -261,7 +261,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_absorbed_kernel(Dec
       alpha[h] = al;  // (four waves and sixteen lanes, the same value)
       uint16_t* dst = pbuf + ((size_t)pb16 * 64 + h + 32 * (n16 >> 3)) * 8 + (n16 & 7);
 #pragma unroll
-      for (int g = 0; g < N; ++g) dst[g * 2048] = f16_bits(__builtin_amdgcn_ldexpf(e, (int)ub[g] - 127));
+      for (int g = 0; g < N; ++g) dst[g * 2048] = f16_bits(below_f16_max(__builtin_amdgcn_ldexpf(e, (int)ub[g] - 127)));
     }
     dma_barrier<2 * kKCopies + kVCopies>();  // weights in place; this page's V has landed (younger: two K, one V)
     // ---- o = alpha o + P' codes

@@ -261,7 +261,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
     const uint32_t t2 = sm.ub[2] > sm.ub[3] ? sm.ub[2] : sm.ub[3];
     top = top > t2 ? top : t2;
     top = top > 127 + kLeastExp ? top : 127 + kLeastExp;
-    sm.mx = sm.s + ((float)top - 127.f);
+    sm.mx = sm.s + ((float)top - (127.f + kTopExp));
   };
   auto softmax_rows = [&](Softmax& sm) {
     sm.mx = row_max_step<0>(sm.mx);
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
     uint16_t* dst = pbuf + ((size_t)((l >> 5) * 64 + sm_h[u] + 16 * ((l & 31) >> 3)) * 8 + (l & 7));
 #pragma unroll
     for (int g = 0; g < 4; ++g)  // (groups past the rank: filed, not read)
-      dst[g * 1024] = f16_bits(__builtin_amdgcn_ldexpf(sm.e, (int)sm.ub[g] - 127));
+      dst[g * 1024] = f16_bits(below_f16_max(__builtin_amdgcn_ldexpf(sm.e, (int)sm.ub[g] - 127)));
   };
   struct Query {
     double turns;

@@ -246,7 +246,7 @@ __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeP
     uint32_t top = 127 + kLeastExp;
 #pragma unroll
     for (int g = 0; g < 8; ++g) top = top > sm.ub[g] ? top : sm.ub[g];
-    sm.mx = sm.s + ((float)top - 127.f);
+    sm.mx = sm.s + ((float)top - (127.f + kTopExp));
   };
   auto softmax_rows = [&](Softmax& sm) {
     sm.mx = row_max_step<0>(sm.mx);
@@ -266,7 +266,7 @@ __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeP
   auto softmax_store = [&](const Softmax& sm, int u) {
     uint16_t* dst = pbuf + (size_t)(sm_h[u] + 16 * (l32 >> 3)) * 8 + (l32 & 7);
 #pragma unroll
-    for (int g = 0; g < 8; ++g) dst[g * 512] = f16_bits(__builtin_amdgcn_ldexpf(sm.e, (int)sm.ub[g] - 127));  // (groups past the rank: filed, not read)
+    for (int g = 0; g < 8; ++g) dst[g * 512] = f16_bits(below_f16_max(__builtin_amdgcn_ldexpf(sm.e, (int)sm.ub[g] - 127)));  // (groups past the rank: filed, not read)
   };
   struct Query {
     double turns;

@@ -6,7 +6,10 @@
 
 namespace lorc {
 
-constexpr int kLeastExp = -40;  // a value scale counts as at least 2^kLeastExp in the softmax reference (see lorc_decode_q8.hip)
+// Of the softmax reference (see lorc_decode_q8.hip): a value scale counts as at least 2^kLeastExp, and the largest weight times scale is 2^kTopExp.
+constexpr int kLeastExp = -40, kTopExp = 15;
+// A weight times scale, below the largest fp16.  (It is at most 2^kTopExp but where fp32 rounds the reference by a unit: scores of 2^24 and more.)
+__device__ __forceinline__ float below_f16_max(float w) { return __builtin_amdgcn_fmed3f(w, 0.f, 65504.f); }
 
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
