@@ -28,9 +28,9 @@ constexpr double kTurns = 0.15915494309189533576888;  // 1 / 2 pi
 // One workgroup of four waves per (sequence, context split, block of 32 query heads), 32 positions at a time.  The step's K codes are
 // widened once into LDS (bf16, operand order), wave w takes every fourth k-step of the scores, partial scores meet in LDS, eight lanes
 // per head take the softmax, and wave w owns every fourth block of 32 value latents, whose codes it loads itself, ahead of the scores.
-// Bound by the chain of four phases and their barriers, one workgroup per compute unit: rank 1024, 16 x 4096 positions 118 us with the merge
-// (bf16 pages, twice the bytes: 90).  The kernel for ranks up to 512 keeps two buffers of pages in LDS, which do not fit here; where both
-// can serve (16 x 8192, rank 512) it takes 40 us and a form like this one 172.
+// Bound by the chain of four phases and the three barriers between them, one workgroup per compute unit: rank 1024, 16 x 4096 positions 118 us with the merge
+// (bf16 pages, twice the bytes: 90).  The kernel for ranks up to 512 keeps two buffers of whole pages in LDS, which do not fit here (two of half
+// pages would: that form is not built); where both can serve (16 x 8192, rank 512) it takes 42 us and a form like this one 172.
 __global__ __launch_bounds__(256, 1) void decode_q8_kernel(DecodeParams p) {
   constexpr int T = 32, NBW = 8;
   extern __shared__ __align__(16) unsigned char smem[];
@@ -189,7 +189,7 @@ __global__ __launch_bounds__(256, 1) void decode_q8_kernel(DecodeParams p) {
 // coordinates, so that row r of block b is position (coordinate) 2 r + b of the step and a lane's eight scores are those of eight
 // consecutive positions, which is what it holds of V.  Keys take the angles of their offset in the step, constants in fp16 like the
 // keys themselves; the base goes to the queries (one frequency per lane, handed round through LDS).
-// Bound by the page stream: 16 x 4096 positions of 2 KiB in 29.6 us, 4.5 TB/s (bf16 pages: 46 us), the merge 4.5 more.
+// Bound by the page stream: 16 x 4096 positions of 2 KiB in 28.9 us, 4.7 TB/s (bf16 pages: 46 us), the merge 4.8 more.
 template <bool BOTH>
 __global__ __launch_bounds__(256, 2) void decode_plain_q8_kernel(DecodeParams p) {
   constexpr int HD = 128, HALF = 64, T = 32;

@@ -7,8 +7,8 @@
 // bits), made once.  So a score is complete in one wave and only row maxima are exchanged.  Weights carry the values' scales (see
 // lorc_decode_q8.hip); wave w owns 64 value latents for all heads.
 //
-// Rank 512, 32 heads, 16 x 8192 positions: 32.4 us, 4.1 TB/s of pages (bf16 pages, twice the bytes: 52), the merge 8 more; 64 heads 57 us with
-// the merge (144).  Short lists are a chain of launch, page id, page, softmax, store: 3 x 2000 positions, rank 384: 11.3 us + 6.4.
+// Rank 512, 32 heads, 16 x 8192 positions: 33 us, 4.0 TB/s of pages (bf16 pages, twice the bytes: 52), the merge 8 more; 64 heads 57 us with
+// the merge (144).  Short lists are a chain of launch, page id, page, softmax, store: 3 x 2000 positions, rank 384: 11.4 us + 5.7.
 #include "lorc_device.h"
 #include "lorc_kernels.h"
 #include "lorc_q8.h"

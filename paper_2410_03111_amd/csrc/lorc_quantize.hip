@@ -9,8 +9,8 @@
 // tile.  K: a lane's elements belong to one position, a group is eight tiles and the two halves of the wave.  V: a lane's
 // elements are eight positions of one latent, a group is four tiles and the 32 lanes of a half.  Either way the maximum of a
 // group stays inside one wave, and a page is 2 (groups of K) + 4 (groups of V) units of work, one wave each.
-// Bound by memory: 2 bytes read and 1 written per latent (+ 1 per 128).  4 prompts of 8192 positions, rank 512: 20 us, 5.1 TB/s; one token of
-// each of 64 sequences: 5.9 us, the chain position -> page id -> latents -> maximum -> codes.
+// Bound by memory: 2 bytes read and 1 written per latent (+ 1 per 128).  4 prompts of 8192 positions, rank 512: 19 us, 5.2 TB/s; one token of
+// each of 64 sequences: 6.0 us, the chain position -> page id -> latents -> maximum -> codes.
 #include "lorc_device.h"
 #include "lorc_kernels.h"
 #include "lorc_q8.h"
