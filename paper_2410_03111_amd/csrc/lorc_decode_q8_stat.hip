@@ -108,7 +108,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void decode_q8_stationary_kernel(D
     for (int s = 0; s < NS; ++s)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        // (past the end: zeros; in the lane offset, which is what the bound is compared with)
+        // (past the end: zeros)
         const uint32_t at = real && s < steps ? (uint32_t)((block * steps + s) * 2 + u) * 2048u + lane * 16u : 0x7fff0000u;
         const u32x4 a = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0));
         const u32x4 b = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at + 1024u, 0, 0));

@@ -108,7 +108,7 @@ __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeP
     for (int s = 0; s < NS; ++s)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        // (past the end: zeros; in the lane offset, which is what the bound is compared with)
+        // (past the end: zeros)
         const uint32_t at = real && s < steps ? (uint32_t)((block * steps + s) * 2 + u) * 2048u + lane * 16u : 0x7fff0000u;
         const u32x4 a = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0));
         const u32x4 b = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at + 1024u, 0, 0));
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(kWideThreads, 1) void decode_q8_wide_kernel(DecodeP
   const uint32_t lane4 = 4u * (uint32_t)lane, lane16 = 16u * (uint32_t)lane;
   constexpr int NKC = (2 * NS + NW - 1) / NW, NVC = VB;  // copies per wave, and two of scale bytes each
   auto copy_scales = [&](const u32x4& r, int part, int buf, int i) {  // part: 0 K, 1 V
-    // (the place in the lane offset: of few groups the second block begins behind the page, where a scalar offset is not checked)
+    // (of few groups the second block begins behind the page: its lanes read zeros, the bound counts lane and scalar offset)
     const uint32_t from = 64u * (uint32_t)(r_k + r_v + (part ? gk : 0)) + 256u * (uint32_t)i;
     dma_256(r, uniform_u32(s_lds + (uint32_t)((2 * part + buf) * kWideScales + 256 * i)), lane4 + from, 0u);
   };
